@@ -448,6 +448,76 @@ SBNN_API sbnn_status sbnn_mobilenet_v1_free(sbnn_mbv1* net);
 SBNN_API sbnn_status sbnn_head_noalloc(const sbnn_packed* fc, const float* x_dev, float* logits_dev,
                                        int N, int HW, void* cuda_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Microscaled 4-bit floating point.  The engine that the paper describes computes on bytes and on pruned weights (Sections 3.1
+ * and 3.5); here dense pointwise layers are held in half a byte a weight instead.
+ *
+ * A matrix [M][K] in this form: every 32 consecutive channels of a row (the last block of a row may be shorter) share a scale
+ * 2^(byte - 127), with byte = max(floor(log2(largest magnitude)) + 125, 0), and are rounded to e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * times the scale, and a sign; to nearest, ties to the even code; larger quotients, up to 8, to 6).  A block that holds an
+ * infinity or a NaN gets byte 255 and stands for 32 NaN.
+ *   codes   [M][16 * ceil(K/32)] bytes, the element of the lower index in the lower half of a byte; elements behind K are 0
+ *   scales  tiles of 128 rows x 4 blocks.  The byte of row r, block b is at
+ *           ((r/128) * ceil(K/128) + b/4) * 512 + (r%32) * 16 + ((r%128)/32) * 4 + b%4;
+ *           blocks of a tile that lie behind K are 0, bytes of rows behind M are neither written nor used.
+ * sbnn_mxfp4_bytes: the sizes of the two (host arithmetic only).
+ * sbnn_mxfp4_quantize: x_dev [M] rows of K elements, ldx elements apart, to that form.
+ * sbnn_mxfp4_dequantize: back, rounded to y's type; nothing is written behind a row's K elements.
+ * Strides are in elements and any number from K up; all pointers are 16-byte aligned.  K at least 1; M = 0 returns SBNN_OK.
+ * ------------------------------------------------------------------------------------------------ */
+enum { SBNN_F32 = 0, SBNN_F16 = 1, SBNN_BF16 = 2 }; /* element types of the entry points below */
+
+SBNN_API sbnn_status sbnn_mxfp4_bytes(int M, int K, int64_t* codes_bytes, int64_t* scales_bytes);
+SBNN_API sbnn_status sbnn_mxfp4_quantize(const void* x_dev, int x_type, int64_t ldx, uint8_t* codes_dev, uint8_t* scales_dev,
+                                         int M, int K, void* cuda_stream);
+SBNN_API sbnn_status sbnn_mxfp4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, void* y_dev, int y_type,
+                                           int64_t ldy, int M, int K, void* cuda_stream);
+
+/*
+ * 1x1 convolution (a linear layer over M pixels or tokens) on 4-bit operands:
+ *   Y[m][o] = act( bias[o] + sum_k Wq[o][k] * Xq[m][k] )
+ * with Wq and Xq the values that the 4-bit forms stand for.  Products and the scales are exact; they are summed in fp32 on the
+ * tensor cores; bias and ReLU are fp32; the result is rounded once, to y's type.
+ *   w_codes_dev, w_scales_dev  the weights [Cout][Cin] in the form above (sbnn_mxfp4_quantize makes it)
+ *   bias_dev                   [Cout] fp32 or NULL
+ *   x_dev                      [M] rows of Cin elements of x_type, ldx apart; rounded to 4 bits inside the call
+ *   y_dev                      [M] rows of Cout elements of y_type, ldy apart
+ *   flags                      SBNN_RELU or 0
+ *   workspace_dev              device memory for the rounded activations, the two sizes of sbnn_mxfp4_bytes(M, Cin) added; of
+ *                              the caller, so that calls in flight at the same time, and graphs, can have their own.  Not used,
+ *                              and may be NULL, for M <= SBNN_MXFP4_DIRECT_ROWS.
+ * sbnn_conv1x1_mxfp4_q takes activations that are in 4-bit form already (several layers on the same activations round them once).
+ * A pixel's result does not depend on other pixels' values; the order of its sums depends on M, Cin and Cout alone.  A NaN block
+ * makes every output that it meets NaN (0 after ReLU, as max(NaN, 0) is everywhere in this library).
+ * Nothing is allocated or kept between calls.
+ */
+#define SBNN_MXFP4_DIRECT_ROWS 32
+SBNN_API sbnn_status sbnn_conv1x1_mxfp4(const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, const float* bias_dev,
+                                        const void* x_dev, int x_type, int64_t ldx, void* y_dev, int y_type, int64_t ldy,
+                                        int M, int Cin, int Cout, int flags, void* workspace_dev, int64_t workspace_bytes,
+                                        void* cuda_stream);
+SBNN_API sbnn_status sbnn_conv1x1_mxfp4_q(const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, const float* bias_dev,
+                                          const uint8_t* x_codes_dev, const uint8_t* x_scales_dev, void* y_dev, int y_type,
+                                          int64_t ldy, int M, int Cin, int Cout, int flags, void* cuda_stream);
+
+/*
+ * What a classifier answers: log probabilities of given classes, entropy and the most probable classes of rows of logits.
+ *   logits_dev    [rows] rows of `classes` elements of `type`, ld elements apart (any ld from classes up)
+ *   targets_dev   [rows][ntargets] int32 classes; logprob_dev [rows][ntargets] fp32: their log probabilities.  A negative class
+ *                 asks for nothing and gets 0; one from `classes` up gets NaN.  Both may be NULL if ntargets = 0.
+ *   entropy_dev   [rows] fp32, -sum p log p in nats, or NULL
+ *   top           number of most probable classes wanted, 0 to SBNN_LOGPROBS_MAX_TOP and not more than `classes`;
+ *   top_index_dev [rows][top] int32, top_logprob_dev [rows][top] fp32: those classes, most probable first, of equal ones the
+ *                 lower index first, and their log probabilities.  Both may be NULL if top = 0.
+ * Classes at -inf have probability 0 (log probability -inf).  Rows without a class above -inf, and rows with a logit of +inf or
+ * NaN, have no distribution: their log probabilities and entropy are NaN.  Their most probable classes are still those
+ * with the largest logits, where a NaN counts as -inf.  Sums are fp32.  One kernel; nothing is allocated.
+ */
+#define SBNN_LOGPROBS_MAX_TOP 32
+SBNN_API sbnn_status sbnn_logprobs(const void* logits_dev, int type, int64_t ld, int rows, int classes, const int32_t* targets_dev,
+                                   int ntargets, float* logprob_dev, float* entropy_dev, int top, int32_t* top_index_dev,
+                                   float* top_logprob_dev, void* cuda_stream);
+
 /*
  * Synchronise the stream and report device-side trouble: SBNN_ERR_CUDA if a kernel failed,
  * SBNN_ERR_TIMEOUT if a bounded wait inside a kernel expired, else SBNN_OK.

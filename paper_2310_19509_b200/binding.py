@@ -8,6 +8,7 @@ import numpy as np
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 SBNN_RELU, SBNN_BF16_TC, SBNN_OUT_CM, SBNN_BF16_GATHER = 1, 2, 4, 8
+SBNN_F32, SBNN_F16, SBNN_BF16 = 0, 1, 2
 _lib = None
 
 
@@ -38,7 +39,7 @@ def lib():
         raise ImportError(f"{path} not found: build it with `python -m paper_2310_19509_b200.build`; "
                           "there is no fallback implementation")
     L = C.CDLL(path)
-    P, I = C.c_void_p, C.c_int
+    P, I, L64 = C.c_void_p, C.c_int, C.c_int64
     sig = {
         "sbnn_pack_weights": [P, P, P, I, I, I, I, I, P],
         "sbnn_pack_weights_pattern": [P, P, P, I, I, I, I, I, P],
@@ -69,6 +70,12 @@ def lib():
         "sbnn_mobilenet_v1_free": [P],
         "sbnn_get_async_status": [P],
         "sbnn_head_noalloc": [P, P, P, I, I, P],
+        "sbnn_mxfp4_bytes": [I, I, P, P],
+        "sbnn_mxfp4_quantize": [P, I, L64, P, P, I, I, P],
+        "sbnn_mxfp4_dequantize": [P, P, P, I, L64, I, I, P],
+        "sbnn_conv1x1_mxfp4": [P, P, P, P, I, L64, P, I, L64, I, I, I, I, P, L64, P],
+        "sbnn_conv1x1_mxfp4_q": [P, P, P, P, P, P, I, L64, I, I, I, I, P],
+        "sbnn_logprobs": [P, I, L64, I, I, P, I, P, P, I, P, P, P],
         "sbnn_selftest_wait_timeout": [P],
         "sbnn_prepare": [P, I, I, I, I],
         "sbnn_selftest_fma_rate": [I, P, P],
@@ -279,6 +286,54 @@ def avgpool(x, y, n, hw, c, stream=None):
 def head_noalloc(fc: Packed, x, logits, n, hw, stream=None):
     """Average pool + classifier through the library's fixed scratch array; allocates nothing."""
     _check(lib().sbnn_head_noalloc(fc.handle, _ptr(x), _ptr(logits), n, hw, _stream(stream)))
+
+
+_ELEMENT_TYPES = {}
+
+
+def _type(t):
+    """The SBNN_F32 / F16 / BF16 of a torch tensor."""
+    if not _ELEMENT_TYPES:
+        import torch
+        _ELEMENT_TYPES.update({torch.float32: SBNN_F32, torch.float16: SBNN_F16, torch.bfloat16: SBNN_BF16})
+    code = _ELEMENT_TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"fp32, fp16 or bf16 elements are taken, not {t.dtype}")
+    return code
+
+
+def mxfp4_bytes(m, k):
+    """(bytes of the codes, bytes of the scales) of an [m][k] matrix in microscaled 4-bit form."""
+    codes, scales = C.c_int64(), C.c_int64()
+    _check(lib().sbnn_mxfp4_bytes(m, k, C.byref(codes), C.byref(scales)))
+    return codes.value, scales.value
+
+
+def mxfp4_quantize(x, ldx, codes, scales, m, k, stream=None):
+    """x: a tensor of fp32, fp16 or bf16, rows of k elements ldx apart; codes and scales: uint8, of mxfp4_bytes(m, k)."""
+    _check(lib().sbnn_mxfp4_quantize(_ptr(x), _type(x), ldx, _ptr(codes), _ptr(scales), m, k, _stream(stream)))
+
+
+def mxfp4_dequantize(codes, scales, y, ldy, m, k, stream=None):
+    _check(lib().sbnn_mxfp4_dequantize(_ptr(codes), _ptr(scales), _ptr(y), _type(y), ldy, m, k, _stream(stream)))
+
+
+def conv1x1_mxfp4(w_codes, w_scales, bias, x, ldx, y, ldy, m, cin, cout, flags=SBNN_RELU, workspace=None, stream=None):
+    """1x1 layer on 4-bit weights, activations rounded to 4 bits inside; workspace: uint8, for m > 32 (see sbnn_conv1x1_mxfp4)."""
+    _check(lib().sbnn_conv1x1_mxfp4(_ptr(w_codes), _ptr(w_scales), _ptr(bias), _ptr(x), _type(x), ldx, _ptr(y), _type(y), ldy, m, cin, cout,
+                                    flags, _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream(stream)))
+
+
+def conv1x1_mxfp4_q(w_codes, w_scales, bias, x_codes, x_scales, y, ldy, m, cin, cout, flags=SBNN_RELU, stream=None):
+    """The same on activations that are in 4-bit form already."""
+    _check(lib().sbnn_conv1x1_mxfp4_q(_ptr(w_codes), _ptr(w_scales), _ptr(bias), _ptr(x_codes), _ptr(x_scales), _ptr(y), _type(y), ldy, m, cin,
+                                      cout, flags, _stream(stream)))
+
+
+def logprobs(logits, ld, rows, classes, targets, ntargets, logprob, entropy, top, top_index, top_logprob, stream=None):
+    """Log probabilities of `targets` (int32 [rows][ntargets]), entropy and the `top` most probable classes of rows of logits."""
+    _check(lib().sbnn_logprobs(_ptr(logits), _type(logits), ld, rows, classes, _ptr(targets), ntargets, _ptr(logprob), _ptr(entropy), top,
+                               _ptr(top_index), _ptr(top_logprob), _stream(stream)))
 
 
 def prepare(w: Packed, n, h, wd, flags=0):

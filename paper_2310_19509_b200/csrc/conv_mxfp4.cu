@@ -1,0 +1,459 @@
+// 1x1 convolution on microscaled 4-bit operands (layout: mxfp4.cuh), fp32 sums on the tensor cores.
+//
+//   y[m][o] = act( bias[o] + sum_b 2^(ex(m,b) + ew(o,b)) sum_{k in block b} cx(m,k) cw(o,k) )
+//
+// The tensor core multiplies e2m1 codes and applies the two scales of every 32 channels itself (kind::mxf4).  Weights are its
+// A operand: a tile is 128 output channels (the lanes of tensor memory) x BN pixels (its columns), so
+//   - the few pixels of a single token or a small batch are a narrow N (8 to 32) and the weights, which are what such a call
+//     reads, pass through the wide operand once;
+//   - a warp of the epilogue holds 32 consecutive channels of a pixel and stores them without a transposition.
+// Both operands arrive by tiled copies (128-byte rows = 256 channels, 128-byte swizzle), scales by linear copies of their
+// tiles and from shared into tensor memory by tcgen05.cp.  A pipeline stage keeps tensor-memory columns for its scales of its
+// own, so that a copy into them never meets an MMA that still reads them.
+// Calls of up to 32 pixels are rounded to 4 bits by the CTAs themselves (FUSED): one launch, and the rounding happens while
+// the first weights are on their way.
+// Where tiles are fewer than SMs the channel steps of a tile are shared by the CTAs of a cluster, which add up their sums
+// through each other's shared memory in the order of their ranks: results do not depend on timing.
+#include <cuda.h>
+
+#include <algorithm>
+
+#include "common.h"
+#include "mxfp4.cuh"
+#include "pipeline.cuh"
+#include "tcgen05.cuh"
+
+namespace sbnn {
+
+sbnn_status mxfp4_quantize_launch(const void* x, int x_type, int64_t ldx, uint8_t* codes, uint8_t* scales, int M, int K, cudaStream_t st);
+
+namespace {
+
+constexpr int kThreads = 256;       // warp 0 copies, warp 1 issues MMAs, warps 4-7 drain; warps 2-7 round activations (FUSED)
+constexpr int kStep = 256;          // channels of a pipeline step: 128 bytes of codes a row
+constexpr int kABytes = 128 * 128;  // the weights of a step
+constexpr int kMaxStages = 8;
+constexpr int kFusedPixels = SBNN_MXFP4_DIRECT_ROWS;
+constexpr int kMaxSmem = 227 * 1024;
+
+struct Args {
+    const uint8_t *w_scales, *x_scales;
+    const float* bias;
+    const void* x;          // FUSED: the activations as they are
+    void* y;
+    int64_t ldx, ldy;
+    int x_type, y_type;
+    int M, Cout, K;
+    int bn;                 // pixels of a tile
+    int ctiles;             // tiles of 128 output channels
+    int steps, split;       // steps of a tile, CTAs that share them
+    int stages;
+    int relu;
+    int vec;                // FUSED: rows of x can be read 16 bytes at a time
+    int* status;
+};
+
+struct Shared {
+    uint64_t full[kMaxStages], empty[kMaxStages], done, ready;
+    uint32_t tmem;
+    int abort;
+};
+
+// What a launch needs of shared memory, by parts (all multiples of 1024 bytes except the last).
+struct Layout {
+    int a, b, sfa, sfb;     // a stage's operands; FUSED: b and sfb are those of one step and all steps of the CTA stay
+    int stage, resident, total;
+};
+__host__ __device__ inline Layout layout_of(int bn, int stages, int steps, bool fused) {
+    Layout l;
+    l.a = kABytes;
+    l.b = bn * 128;
+    l.sfa = 1024;
+    l.sfb = 1024 * ((bn + 127) / 128);
+    l.stage = l.a + l.sfa + (fused ? 0 : l.b + l.sfb);
+    l.resident = fused ? steps * (l.b + l.sfb) : 0;
+    l.total = stages * l.stage + l.resident + 1024 + (int)sizeof(Shared);
+    return l;
+}
+// Columns of tensor memory: sums, then the scales of the stages.
+__host__ __device__ constexpr int sf_columns(int bn) { return 8 + 8 * ((bn + 127) / 128); }
+__host__ __device__ inline uint32_t tmem_columns(int bn, int stages) {
+    const int need = (bn + 31) / 32 * 32 + stages * sf_columns(bn);
+    uint32_t c = 32;
+    while ((int)c < need) c *= 2;
+    return c;
+}
+
+// ---- block-scaled MMA ------------------------------------------------------------------------------
+// Instruction descriptor: e2m1 x e2m1 -> fp32, both K-major, M = 128, N = n, scales are powers of two (ue8m0), two a row and
+// MMA; `half` says which two of the four bytes of a scale word.
+__device__ __forceinline__ uint32_t mx_instr_desc(int n, int half) {
+    return ((uint32_t)(2 * half) << 4)         // B: scale factor id 0 or 2
+           | (1u << 7) | (1u << 10)            // A and B: e2m1
+           | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(128 >> 7) << 27)
+           | ((uint32_t)(2 * half) << 29);     // A: scale factor id
+}
+__device__ __forceinline__ void umma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+}
+// 512 bytes of scales (32 lanes x 16 bytes, linear) into 4 columns, the same in each quarter of the lanes.
+__device__ __forceinline__ void scales_to_tmem(uint32_t tmem, uint32_t smem) {
+    uint64_t d = (uint64_t)((smem & 0x3FFFFu) >> 4);
+    d |= (uint64_t)1 << 16;            // leading byte offset: not used, rows are 16 bytes
+    d |= (uint64_t)(128 >> 4) << 32;   // groups of 8 rows are 128 bytes apart
+    d |= (uint64_t)1 << 46;            // descriptor version; no swizzle
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(d) : "memory");
+}
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void store_remote(uint32_t addr, uint32_t rank, float v) {
+    asm volatile("{\n\t.reg .b32 r;\n\t"
+                 "mapa.shared::cluster.u32 r, %0, %1;\n\t"
+                 "st.shared::cluster.f32 [r], %2;\n\t}" ::"r"(addr), "r"(rank), "f"(v) : "memory");
+}
+
+// Polls without regard to the abort flag, a bounded number of times: what is in flight when a CTA gives up has to land first.
+__device__ __forceinline__ void land(uint64_t* bar, uint32_t parity) {
+    for (uint32_t i = 0; i < kWaitLimit && !mbar_try_wait(bar, parity); ++i) __nanosleep(64);
+}
+
+// ---- activations of a FUSED call: rounded by the CTA for the steps that it sums -------------------------
+template <class T, bool VEC>
+__device__ __forceinline__ void round_block(const T* p, int n, uint4& codes, uint32_t& byte) {
+    Eight<T> e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load8<VEC>(e[i], p + 8 * i, n - 8 * i);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = max(m, largest_bits(e[i]));
+    byte = mx_scale_byte(m);
+    codes = make_uint4(encode8(e[0], byte), encode8(e[1], byte), encode8(e[2], byte), encode8(e[3], byte));
+}
+template <class T>
+__device__ __forceinline__ void round_pixels(const Args& a, uint8_t* b, uint8_t* sfb, int b_bytes, int sfb_bytes, int step0, int steps, int t, int nt) {
+    const int blocks = steps * 8;
+    const T* x = static_cast<const T*>(a.x);
+    for (int i = t; i < a.M * blocks; i += nt) {
+        const int row = i / blocks, blk = i % blocks, s = blk >> 3, c = blk & 7, k = (step0 * 8 + blk) * 32, n = a.K - k;
+        uint4 codes = make_uint4(0, 0, 0, 0);
+        uint32_t byte = 0;
+        if (n > 0) {
+            const T* p = x + row * a.ldx + k;
+            if (a.vec && n >= 32)
+                round_block<T, true>(p, 32, codes, byte);
+            else
+                round_block<T, false>(p, n, codes, byte);
+        }
+        *reinterpret_cast<uint4*>(b + s * b_bytes + row * 128 + ((c ^ (row & 7)) << 4)) = codes;
+        sfb[s * sfb_bytes + (c >> 2) * 512 + row * 16 + (c & 3)] = (uint8_t)byte;   // row < 32
+    }
+}
+
+// ---- epilogue: one output channel a lane ---------------------------------------------------------------
+template <class T>
+__device__ __forceinline__ void store_pixel(T* y, int64_t ldy, int64_t m, int o, float v) { y[m * ldy + o] = from_float<T>(v); }
+__device__ __forceinline__ void store_any(const Args& a, int64_t m, int o, float v) {
+    if (a.y_type == SBNN_F32) store_pixel(static_cast<float*>(a.y), a.ldy, m, o, v);
+    else if (a.y_type == SBNN_F16) store_pixel(static_cast<__half*>(a.y), a.ldy, m, o, v);
+    else store_pixel(static_cast<__nv_bfloat16*>(a.y), a.ldy, m, o, v);
+}
+
+template <bool FUSED>
+__global__ void __launch_bounds__(kThreads, 1)
+conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const Args a) {
+    extern __shared__ uint8_t raw[];
+    uint8_t* const base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    const Layout l = layout_of(a.bn, a.stages, (a.steps + a.split - 1) / a.split, FUSED);
+    uint8_t* const resident = base + a.stages * l.stage;
+    Shared& sh = *reinterpret_cast<Shared*>(resident + l.resident);
+    // operands first, scales behind them: the operands of every stage start on 1024 bytes
+    uint8_t* const scales = base + a.stages * (l.a + (FUSED ? 0 : l.b));
+    const int op_stage = l.a + (FUSED ? 0 : l.b), sf_stage = l.sfa + (FUSED ? 0 : l.sfb);
+    uint8_t* const resident_sf = resident + (l.resident / (l.b + l.sfb)) * l.b;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int tile = blockIdx.x / a.split, rank = a.split > 1 ? (int)cluster_rank() : 0;
+    const int ct = tile % a.ctiles, n0 = tile / a.ctiles * a.bn;
+    const int step0 = (int)((int64_t)a.steps * rank / a.split), step1 = (int)((int64_t)a.steps * (rank + 1) / a.split), steps = step1 - step0;
+    const int ktiles = mx_ktiles(a.K);
+    const int first = n0 & 127, atoms = (first + a.bn + 127) >> 7;   // tiles of scales that the pixels of a tile lie in
+    const int xtiles = (a.M + 127) >> 7;
+    const uint32_t columns = tmem_columns(a.bn, a.stages), sf_cols = (uint32_t)sf_columns(a.bn);
+
+    if (warp == 1) {
+        tmem_alloc(&sh.tmem, columns);
+    } else if (threadIdx.x == 0) {
+        for (int i = 0; i < a.stages; ++i) {
+            mbar_init(&sh.full[i], 1);
+            mbar_init(&sh.empty[i], 1);
+        }
+        mbar_init(&sh.done, 1);
+        mbar_init(&sh.ready, kThreads - 64);
+        mbar_fence_init();
+        sh.abort = 0;
+        prefetch_map(&wmap);
+        if (!FUSED) prefetch_map(&xmap);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = sh.tmem, tmem_sf = tmem + (uint32_t)((a.bn + 31) / 32 * 32);
+    volatile int* const abort = &sh.abort;
+    grid_dependency_wait();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int issued = 0;
+            for (int i = 0; i < steps; ++i, ++issued) {
+                const int s = i % a.stages, round = i / a.stages, ks = step0 + i;
+                if (round && !mbar_wait(&sh.empty[s], (round - 1) & 1, abort, a.status, SBNN_ERR_TIMEOUT)) break;
+                uint8_t* const op = base + s * op_stage;
+                uint8_t* const sf = scales + s * sf_stage;
+                const uint32_t sfbytes = 512u * (uint32_t)min(2, ktiles - 2 * ks);
+                const int rows = FUSED ? 0 : min(atoms, xtiles - (n0 >> 7));
+                mbar_arrive_expect_tx(&sh.full[s], (uint32_t)op_stage + sfbytes * (uint32_t)(1 + rows));
+                tensor_g2s_2d(op, &wmap, ks * 64, ct * 128, &sh.full[s]);
+                bulk_g2s(sf, a.w_scales + ((int64_t)ct * ktiles + 2 * ks) * 512, sfbytes, &sh.full[s]);
+                if (!FUSED) {
+                    tensor_g2s_2d(op + l.a, &xmap, ks * 64, n0, &sh.full[s]);
+                    for (int r = 0; r < rows; ++r)
+                        bulk_g2s(sf + l.sfa + r * 1024, a.x_scales + ((int64_t)((n0 >> 7) + r) * ktiles + 2 * ks) * 512, sfbytes, &sh.full[s]);
+                }
+            }
+            if (*abort)
+                for (int i = max(0, issued - a.stages); i < issued; ++i) land(&sh.full[i % a.stages], (i / a.stages) & 1);
+        }
+    } else if (warp == 1) {
+        bool ok = true;
+        if (FUSED) ok = mbar_wait(&sh.ready, 0, abort, a.status, SBNN_ERR_TIMEOUT);
+        for (int i = 0; ok && i < steps; ++i) {
+            const int s = i % a.stages, ks = step0 + i;
+            if (!(ok = mbar_wait(&sh.full[s], (i / a.stages) & 1, abort, a.status, SBNN_ERR_TIMEOUT))) break;
+            tc_fence_after_sync();
+            const uint32_t op = smem_u32(base + s * op_stage), sf = smem_u32(scales + s * sf_stage);
+            const uint32_t b = FUSED ? smem_u32(resident + i * l.b) : op + l.a, sfb = FUSED ? smem_u32(resident_sf + i * l.sfb) : sf + l.sfa;
+            const uint32_t tsfa = tmem_sf + (uint32_t)s * sf_cols, tsfb = tsfa + 8;
+            const int n64 = min(4, (a.K - ks * kStep + 63) >> 6), pairs = (n64 + 1) >> 1;
+            if (elect_one()) {
+                for (int j = 0; j < pairs; ++j) {
+                    scales_to_tmem(tsfa + 4 * j, sf + 512 * j);
+                    for (int r = 0; r < atoms; ++r) scales_to_tmem(tsfb + 4 * (j * atoms + r), sfb + r * 1024 + 512 * j);
+                }
+                for (int j = 0; j < n64; ++j)
+                    umma_mxf4(tmem, operand_desc(op + 32 * j), operand_desc(b + 32 * j), mx_instr_desc(a.bn, j & 1), tsfa + 4 * (j >> 1),
+                              tsfb + 4 * (j >> 1) * atoms + (first >> 5), (uint32_t)(i | j));
+                umma_commit(&sh.empty[s]);
+                if (i + 1 == steps) umma_commit(&sh.done);
+            }
+            __syncwarp();
+        }
+        if (!ok) {   // the MMAs issued so far end before the tensor memory is given back
+            if (elect_one()) umma_commit(&sh.done);
+            __syncwarp();
+            land(&sh.done, 0);
+        }
+    }
+    if (FUSED && warp >= 2) {
+        const int t = threadIdx.x - 64, nt = kThreads - 64;
+        if (a.x_type == SBNN_F32) round_pixels<float>(a, resident, resident_sf, l.b, l.sfb, step0, steps, t, nt);
+        else if (a.x_type == SBNN_F16) round_pixels<__half>(a, resident, resident_sf, l.b, l.sfb, step0, steps, t, nt);
+        else round_pixels<__nv_bfloat16>(a, resident, resident_sf, l.b, l.sfb, step0, steps, t, nt);
+        fence_async_smem();
+        mbar_arrive(&sh.ready);
+    }
+    bool ok = true;
+    const int quarter = warp & 3, row = quarter * 32 + lane, o = ct * 128 + row;
+    if (warp >= 4) {
+        ok = mbar_wait(&sh.done, 0, abort, a.status, SBNN_ERR_TIMEOUT);
+        tc_fence_after_sync();
+    }
+    if (a.split == 1) {
+        if (warp >= 4 && ok) {
+            const float bias = a.bias && o < a.Cout ? __ldg(a.bias + o) : 0.f;
+            for (int c0 = 0; c0 < a.bn; c0 += 16) {
+                uint32_t v[16];
+                tmem_ld(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c0, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    const int64_t m = (int64_t)n0 + c0 + c;
+                    float f = __uint_as_float(v[c]) + bias;
+                    if (a.relu) f = fmaxf(f, 0.f);
+                    if (c0 + c < a.bn && m < a.M && o < a.Cout) store_any(a, m, o, f);
+                }
+            }
+        }
+    } else {
+        // every CTA of the cluster is done with its stages: their memory takes the sums that the others send
+        __syncwarp();
+        cluster_sync();
+        const int width = (a.bn + a.split - 1) / a.split;
+        float* const exchange = reinterpret_cast<float*>(base);
+        if (warp >= 4 && ok) {
+            const uint32_t ex = smem_u32(exchange);
+            for (int c0 = 0; c0 < a.bn; c0 += 16) {
+                uint32_t v[16];
+                tmem_ld(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c0, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    const int col = c0 + c, owner = col / width;
+                    if (col < a.bn && n0 + col < a.M)
+                        store_remote(ex + (uint32_t)((rank * width + col - owner * width) * 128 + row) * 4u, (uint32_t)owner, __uint_as_float(v[c]));
+                }
+            }
+        }
+        __syncwarp();
+        cluster_sync();
+        if (warp >= 4 && ok) {
+            const float bias = a.bias && o < a.Cout ? __ldg(a.bias + o) : 0.f;
+            for (int c = 0; c < width; ++c) {
+                const int col = rank * width + c;
+                if (col >= a.bn || n0 + col >= a.M) break;
+                float f = 0.f;
+                for (int r = 0; r < a.split; ++r) f += exchange[(r * width + c) * 128 + row];
+                f += bias;
+                if (a.relu) f = fmaxf(f, 0.f);
+                if (o < a.Cout) store_any(a, n0 + col, o, f);
+            }
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, columns);
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+struct Plan {
+    int bn, split, stages;
+    bool fused;
+};
+
+// Tiles of 256 pixels where they fill the SMs, else of 128 or 64, else (up to 32 pixels) one tile as wide as the pixels; the
+// steps of tiles that are still fewer than half the SMs are shared, two steps a CTA at least.
+Plan plan_for(int64_t M, int Cout, int K, bool raw) {
+    const int sms = device_sms(), ctiles = (Cout + 127) / 128, steps = (K + kStep - 1) / kStep;
+    Plan p;
+    p.bn = 64;
+    if (M <= kFusedPixels) p.bn = (int)(M + 7) / 8 * 8;
+    else if (ctiles * ((M + 255) / 256) >= sms) p.bn = 256;
+    else if (ctiles * ((M + 127) / 128) >= sms) p.bn = 128;
+    const int64_t tiles = ctiles * ((M + p.bn - 1) / p.bn);
+    p.split = 1;
+    while (p.split < 8 && tiles * (p.split + 1) <= sms && steps >= 2 * (p.split + 1)) ++p.split;
+    p.fused = false;
+    if (raw && M <= kFusedPixels) {
+        while (p.split < 8 && layout_of(p.bn, 4, (steps + p.split - 1) / p.split, true).total > kMaxSmem) ++p.split;
+        p.fused = layout_of(p.bn, 4, (steps + p.split - 1) / p.split, true).total <= kMaxSmem;
+    }
+    p.stages = p.bn <= 128 ? 6 : 4;
+    while (p.stages > 2 && layout_of(p.bn, p.stages, (steps + p.split - 1) / p.split, p.fused).total > kMaxSmem) --p.stages;
+    return p;
+}
+
+sbnn_status launch(const Args& given, const Plan& p, const uint8_t* w_codes, const uint8_t* x_codes, cudaStream_t st) {
+    Args a = given;
+    sbnn_status r = async_status_word(&a.status);
+    if (r != SBNN_OK) return r;
+    a.bn = p.bn;
+    a.split = p.split;
+    a.stages = p.stages;
+    a.ctiles = (a.Cout + 127) / 128;
+    a.steps = (a.K + kStep - 1) / kStep;
+    const int64_t ctas = (int64_t)a.ctiles * (((int64_t)a.M + a.bn - 1) / a.bn) * a.split;
+    if (ctas > 0x7fffffff) return fail(SBNN_ERR_SHAPE, "too many tiles");
+    CUtensorMap wmap, xmap;
+    const unsigned long long row_bytes = 16ull * mx_blocks(a.K), strides[1] = {row_bytes};
+    const unsigned long long wdims[2] = {row_bytes / 2, (unsigned long long)a.Cout}, xdims[2] = {row_bytes / 2, (unsigned long long)a.M};
+    const unsigned wbox[2] = {64, 128}, xbox[2] = {64, (unsigned)a.bn};
+    if ((r = encode_tiled_map(&wmap, w_codes, 2, 2, wdims, strides, wbox, 128)) != SBNN_OK) return r;
+    if (p.fused) xmap = wmap;
+    else if ((r = encode_tiled_map(&xmap, x_codes, 2, 2, xdims, strides, xbox, 128)) != SBNN_OK) return r;
+    auto* const kernel = p.fused ? conv_mxfp4_kernel<true> : conv_mxfp4_kernel<false>;
+    if ((r = set_max_dyn_smem(reinterpret_cast<const void*>(kernel), kMaxSmem)) != SBNN_OK) return r;
+    const size_t smem = (size_t)layout_of(a.bn, a.stages, (a.steps + a.split - 1) / a.split, p.fused).total;
+    SBNN_CUDA_TRY(launch_kernel_cluster(kernel, dim3((unsigned)ctas), dim3(kThreads), smem, st, (unsigned)a.split, wmap, xmap, a));
+    return SBNN_OK;
+}
+
+sbnn_status check_call(const uint8_t* w_codes, const uint8_t* w_scales, const float* bias, const void* y, int y_type, int64_t ldy, int M, int Cin,
+                       int Cout, int flags) {
+    if (M < 0 || Cin <= 0 || Cout <= 0) return fail(SBNN_ERR_SHAPE, "bad shape M=%d Cin=%d Cout=%d", M, Cin, Cout);
+    if (y_type != SBNN_F32 && y_type != SBNN_F16 && y_type != SBNN_BF16) return fail(SBNN_ERR_UNSUPPORTED, "y_dev: unknown element type %d", y_type);
+    if (ldy < Cout) return fail(SBNN_ERR_SHAPE, "y_dev: rows of %d elements do not fit a stride of %lld", Cout, (long long)ldy);
+    if (flags & ~SBNN_RELU) return fail(SBNN_ERR_UNSUPPORTED, "unknown flag bits 0x%x", flags);
+    if (!aligned16(w_codes) || !aligned16(w_scales) || !aligned16(bias) || !aligned16(y))
+        return fail(SBNN_ERR_ALIGN, "device pointers must be 16-byte aligned");
+    return SBNN_OK;
+}
+
+}  // namespace
+}  // namespace sbnn
+
+using namespace sbnn;
+
+extern "C" sbnn_status sbnn_conv1x1_mxfp4_q(const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, const float* bias_dev,
+                                            const uint8_t* x_codes_dev, const uint8_t* x_scales_dev, void* y_dev, int y_type, int64_t ldy, int M,
+                                            int Cin, int Cout, int flags, void* cuda_stream) {
+    clear_error();
+    if (!w_codes_dev || !w_scales_dev || !x_codes_dev || !x_scales_dev || !y_dev)
+        return fail(SBNN_ERR_NULL, "weights, activations and y_dev must not be NULL");
+    sbnn_status r = check_call(w_codes_dev, w_scales_dev, bias_dev, y_dev, y_type, ldy, M, Cin, Cout, flags);
+    if (r != SBNN_OK) return r;
+    if (!aligned16(x_codes_dev) || !aligned16(x_scales_dev)) return fail(SBNN_ERR_ALIGN, "device pointers must be 16-byte aligned");
+    if (M == 0) return SBNN_OK;
+    if ((r = check_device()) != SBNN_OK) return r;
+    Args a = {};
+    a.w_scales = w_scales_dev, a.x_scales = x_scales_dev, a.bias = bias_dev, a.y = y_dev, a.ldy = ldy, a.y_type = y_type;
+    a.M = M, a.Cout = Cout, a.K = Cin, a.relu = flags & SBNN_RELU;
+    return launch(a, plan_for(M, Cout, Cin, false), w_codes_dev, x_codes_dev, static_cast<cudaStream_t>(cuda_stream));
+}
+
+extern "C" sbnn_status sbnn_conv1x1_mxfp4(const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, const float* bias_dev, const void* x_dev,
+                                          int x_type, int64_t ldx, void* y_dev, int y_type, int64_t ldy, int M, int Cin, int Cout, int flags,
+                                          void* workspace_dev, int64_t workspace_bytes, void* cuda_stream) {
+    clear_error();
+    if (!w_codes_dev || !w_scales_dev || !x_dev || !y_dev) return fail(SBNN_ERR_NULL, "weights, x_dev and y_dev must not be NULL");
+    sbnn_status r = check_call(w_codes_dev, w_scales_dev, bias_dev, y_dev, y_type, ldy, M, Cin, Cout, flags);
+    if (r != SBNN_OK) return r;
+    if (x_type != SBNN_F32 && x_type != SBNN_F16 && x_type != SBNN_BF16) return fail(SBNN_ERR_UNSUPPORTED, "x_dev: unknown element type %d", x_type);
+    if (ldx < Cin) return fail(SBNN_ERR_SHAPE, "x_dev: rows of %d elements do not fit a stride of %lld", Cin, (long long)ldx);
+    if (!aligned16(x_dev)) return fail(SBNN_ERR_ALIGN, "x_dev must be 16-byte aligned");
+    const int64_t codes = (int64_t)M * 16 * mx_blocks(Cin), scales = ((int64_t)M + 127) / 128 * 512 * mx_ktiles(Cin);
+    if (M > kFusedPixels) {
+        if (!workspace_dev) return fail(SBNN_ERR_NULL, "more than %d pixels need a workspace", kFusedPixels);
+        if (workspace_bytes < codes + scales)
+            return fail(SBNN_ERR_SHAPE, "the workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)(codes + scales));
+        if (!aligned16(workspace_dev)) return fail(SBNN_ERR_ALIGN, "workspace_dev must be 16-byte aligned");
+    }
+    if (M == 0) return SBNN_OK;
+    if ((r = check_device()) != SBNN_OK) return r;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    Args a = {};
+    a.w_scales = w_scales_dev, a.bias = bias_dev, a.y = y_dev, a.ldy = ldy, a.y_type = y_type;
+    a.M = M, a.Cout = Cout, a.K = Cin, a.relu = flags & SBNN_RELU;
+    const Plan p = plan_for(M, Cout, Cin, true);
+    if (p.fused) {
+        a.x = x_dev, a.ldx = ldx, a.x_type = x_type;
+        a.vec = ldx * (x_type == SBNN_F32 ? 4 : 2) % 16 == 0;
+        return launch(a, p, w_codes_dev, nullptr, st);
+    }
+    if (M <= kFusedPixels) return fail(SBNN_ERR_UNSUPPORTED, "Cin=%d is too wide for so few pixels", Cin);
+    uint8_t* const xc = static_cast<uint8_t*>(workspace_dev);
+    a.x_scales = xc + codes;
+    if ((r = mxfp4_quantize_launch(x_dev, x_type, ldx, xc, xc + codes, M, Cin, st)) != SBNN_OK) return r;
+    return launch(a, p, w_codes_dev, xc, st);
+}
