@@ -49,6 +49,7 @@ struct Args {
     int steps, split;       // steps of a tile, CTAs that share them
     int stages;
     int relu;
+    int early;              // the launch before this one in the stream rounds x and has seen the end of all before it
     int vec;                // FUSED: rows of x can be read 16 bytes at a time
     int* status;
 };
@@ -101,12 +102,16 @@ __device__ __forceinline__ void umma_mxf4(uint32_t d, uint64_t a, uint64_t b, ui
         ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
         : "memory");
 }
-// 512 bytes of scales (32 lanes x 16 bytes, linear) into 4 columns, the same in each quarter of the lanes.
-__device__ __forceinline__ void scales_to_tmem(uint32_t tmem, uint32_t smem) {
+// Descriptor of 512 bytes of scales: 32 rows of 16 bytes, linear.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t smem) {
     uint64_t d = (uint64_t)((smem & 0x3FFFFu) >> 4);
     d |= (uint64_t)1 << 16;            // leading byte offset: not used, rows are 16 bytes
     d |= (uint64_t)(128 >> 4) << 32;   // groups of 8 rows are 128 bytes apart
     d |= (uint64_t)1 << 46;            // descriptor version; no swizzle
+    return d;
+}
+// Those into 4 columns, the same in each quarter of the lanes.
+__device__ __forceinline__ void scales_to_tmem(uint32_t tmem, uint64_t d) {
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(d) : "memory");
 }
 
@@ -119,11 +124,18 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void store_remote(uint32_t addr, uint32_t rank, float v) {
-    asm volatile("{\n\t.reg .b32 r;\n\t"
-                 "mapa.shared::cluster.u32 r, %0, %1;\n\t"
-                 "st.shared::cluster.f32 [r], %2;\n\t}" ::"r"(addr), "r"(rank), "f"(v) : "memory");
+// The address that `addr` has in the shared memory of CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t remote_address(uint32_t addr, int rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
 }
+__device__ __forceinline__ void store_remote(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// Pixels of a tile that each CTA of a cluster finishes: a multiple of 4.
+__host__ __device__ constexpr int exchange_width(int bn, int split) { return (bn + 4 * split - 1) / (4 * split) * 4; }
 
 // Polls without regard to the abort flag, a bounded number of times: what is in flight when a CTA gives up has to land first.
 __device__ __forceinline__ void land(uint64_t* bar, uint32_t parity) {
@@ -164,15 +176,50 @@ __device__ __forceinline__ void round_pixels(const Args& a, uint8_t* b, uint8_t*
 
 // ---- epilogue: one output channel a lane ---------------------------------------------------------------
 template <class T>
-__device__ __forceinline__ void store_pixel(T* y, int64_t ldy, int64_t m, int o, float v) { y[m * ldy + o] = from_float<T>(v); }
-__device__ __forceinline__ void store_any(const Args& a, int64_t m, int o, float v) {
-    if (a.y_type == SBNN_F32) store_pixel(static_cast<float*>(a.y), a.ldy, m, o, v);
-    else if (a.y_type == SBNN_F16) store_pixel(static_cast<__half*>(a.y), a.ldy, m, o, v);
-    else store_pixel(static_cast<__nv_bfloat16*>(a.y), a.ldy, m, o, v);
+struct Out {
+    T* y;             // channel `o` of the tile's first pixel
+    int64_t ldy;
+    float bias;
+    int relu, pixels; // pixels of the tile that there are
+    bool mine;        // the lane's channel exists
+    __device__ __forceinline__ void put(T* at, float sum) const {
+        sum += bias;
+        if (relu) sum = fmaxf(sum, 0.f);
+        if (mine) *at = from_float<T>(sum);
+    }
+    template <int N>
+    __device__ __forceinline__ void put(int c, const uint32_t (&v)[N]) const {
+        T* at = y + c * ldy;
+        if (c + N <= pixels) {
+#pragma unroll
+            for (int i = 0; i < N; ++i, at += ldy) put(at, __uint_as_float(v[i]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i, at += ldy)
+                if (c + i < pixels) put(at, __uint_as_float(v[i]));
+        }
+    }
+};
+// Whole warp: columns [c0, c1) of its lanes, a multiple of 8.
+template <class T>
+__device__ __forceinline__ void drain(const Out<T>& out, uint32_t tmem, int c0, int c1) {
+    int c = c0;
+    for (; c + 32 <= c1; c += 32) {
+        uint32_t v[32];
+        tmem_ld(tmem + (uint32_t)c, v);
+        tmem_ld_wait();
+        out.put(c, v);
+    }
+    for (; c < c1; c += 8) {
+        uint32_t v[8];
+        tmem_ld(tmem + (uint32_t)c, v);
+        tmem_ld_wait();
+        out.put(c, v);
+    }
 }
 
-template <bool FUSED>
-__global__ void __launch_bounds__(kThreads, 1)
+template <bool FUSED, class T>
+__global__ void __launch_bounds__(kThreads, 2)
 conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const Args a) {
     extern __shared__ uint8_t raw[];
     uint8_t* const base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
@@ -212,26 +259,43 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     tc_fence_after_sync();
     const uint32_t tmem = sh.tmem, tmem_sf = tmem + (uint32_t)((a.bn + 31) / 32 * 32);
     volatile int* const abort = &sh.abort;
-    grid_dependency_wait();
+    grid_dependency_release();   // every CTA has its tensor memory: what starts now waits for none of it
+    if (warp || !a.early) grid_dependency_wait();
 
     if (warp == 0) {
         if (lane == 0) {
-            int issued = 0;
-            for (int i = 0; i < steps; ++i, ++issued) {
-                const int s = i % a.stages, round = i / a.stages, ks = step0 + i;
-                if (round && !mbar_wait(&sh.empty[s], (round - 1) & 1, abort, a.status, SBNN_ERR_TIMEOUT)) break;
+            int issued = 0, s = 0;
+            uint32_t phase = 1;   // the first round finds every stage empty
+            const int rows = FUSED ? 0 : min(atoms, xtiles - (n0 >> 7));
+            const uint8_t* wsf = a.w_scales + ((int64_t)ct * ktiles + 2 * step0) * 512;
+            const uint8_t* xsf = FUSED ? nullptr : a.x_scales + ((int64_t)(n0 >> 7) * ktiles + 2 * step0) * 512;
+            // Weights do not depend on the launch that rounds the activations (early): those of the first round are on their way
+            // while it still runs.
+            const int ahead = a.early ? min(a.stages, steps) : 0;
+            for (int i = 0; i < ahead; ++i) {
+                const uint32_t sfbytes = 512u * (uint32_t)min(2, ktiles - 2 * (step0 + i));
+                mbar_arrive_expect_tx(&sh.full[i], (uint32_t)op_stage + sfbytes * (uint32_t)(1 + rows));
+                tensor_g2s_2d(base + i * op_stage, &wmap, (step0 + i) * 64, ct * 128, &sh.full[i]);
+                bulk_g2s(scales + i * sf_stage, wsf + i * 1024, sfbytes, &sh.full[i]);
+            }
+            if (a.early) grid_dependency_wait();
+            for (int ks = step0; ks < step1; ++ks, ++issued) {
+                if (issued >= a.stages && !mbar_wait(&sh.empty[s], phase, abort, a.status, SBNN_ERR_TIMEOUT)) break;
                 uint8_t* const op = base + s * op_stage;
                 uint8_t* const sf = scales + s * sf_stage;
                 const uint32_t sfbytes = 512u * (uint32_t)min(2, ktiles - 2 * ks);
-                const int rows = FUSED ? 0 : min(atoms, xtiles - (n0 >> 7));
-                mbar_arrive_expect_tx(&sh.full[s], (uint32_t)op_stage + sfbytes * (uint32_t)(1 + rows));
-                tensor_g2s_2d(op, &wmap, ks * 64, ct * 128, &sh.full[s]);
-                bulk_g2s(sf, a.w_scales + ((int64_t)ct * ktiles + 2 * ks) * 512, sfbytes, &sh.full[s]);
+                if (issued >= ahead) {
+                    mbar_arrive_expect_tx(&sh.full[s], (uint32_t)op_stage + sfbytes * (uint32_t)(1 + rows));
+                    tensor_g2s_2d(op, &wmap, ks * 64, ct * 128, &sh.full[s]);
+                    bulk_g2s(sf, wsf, sfbytes, &sh.full[s]);
+                }
+                wsf += 1024;
                 if (!FUSED) {
                     tensor_g2s_2d(op + l.a, &xmap, ks * 64, n0, &sh.full[s]);
-                    for (int r = 0; r < rows; ++r)
-                        bulk_g2s(sf + l.sfa + r * 1024, a.x_scales + ((int64_t)((n0 >> 7) + r) * ktiles + 2 * ks) * 512, sfbytes, &sh.full[s]);
+                    for (int r = 0; r < rows; ++r) bulk_g2s(sf + l.sfa + r * 1024, xsf + (int64_t)r * ktiles * 512, sfbytes, &sh.full[s]);
+                    xsf += 1024;
                 }
+                if (++s == a.stages) s = 0, phase ^= 1;
             }
             if (*abort)
                 for (int i = max(0, issued - a.stages); i < issued; ++i) land(&sh.full[i % a.stages], (i / a.stages) & 1);
@@ -239,26 +303,37 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     } else if (warp == 1) {
         bool ok = true;
         if (FUSED) ok = mbar_wait(&sh.ready, 0, abort, a.status, SBNN_ERR_TIMEOUT);
+        // Everything that the issuing lane needs is kept by addition: divisions and rebuilt descriptors of a step took longer
+        // than its MMAs (one token, 8192 -> 16384: 25.1 us, like this 17.6).
+        const uint64_t a0 = operand_desc(smem_u32(base)), b0 = operand_desc(FUSED ? smem_u32(resident) : smem_u32(base) + (uint32_t)l.a);
+        const uint64_t sfa0 = scale_desc(smem_u32(scales)), sfb0 = scale_desc(FUSED ? smem_u32(resident_sf) : smem_u32(scales) + (uint32_t)l.sfa);
+        const uint32_t idesc0 = mx_instr_desc(a.bn, 0), idesc1 = mx_instr_desc(a.bn, 1);
+        int s = 0;
+        uint32_t phase = 0;
         for (int i = 0; ok && i < steps; ++i) {
-            const int s = i % a.stages, ks = step0 + i;
-            if (!(ok = mbar_wait(&sh.full[s], (i / a.stages) & 1, abort, a.status, SBNN_ERR_TIMEOUT))) break;
+            if (!(ok = mbar_wait(&sh.full[s], phase, abort, a.status, SBNN_ERR_TIMEOUT))) break;
             tc_fence_after_sync();
-            const uint32_t op = smem_u32(base + s * op_stage), sf = smem_u32(scales + s * sf_stage);
-            const uint32_t b = FUSED ? smem_u32(resident + i * l.b) : op + l.a, sfb = FUSED ? smem_u32(resident_sf + i * l.sfb) : sf + l.sfa;
             const uint32_t tsfa = tmem_sf + (uint32_t)s * sf_cols, tsfb = tsfa + 8;
-            const int n64 = min(4, (a.K - ks * kStep + 63) >> 6), pairs = (n64 + 1) >> 1;
+            const uint64_t ad = a0 + (uint32_t)(s * (op_stage >> 4)), bd = b0 + (uint32_t)(FUSED ? i * (l.b >> 4) : s * (op_stage >> 4));
+            const uint64_t sa = sfa0 + (uint32_t)(s * (sf_stage >> 4)), sb = sfb0 + (uint32_t)(FUSED ? i * (l.sfb >> 4) : s * (sf_stage >> 4));
+            const int n64 = min(4, (a.K - (step0 + i) * kStep + 63) >> 6);
             if (elect_one()) {
-                for (int j = 0; j < pairs; ++j) {
-                    scales_to_tmem(tsfa + 4 * j, sf + 512 * j);
-                    for (int r = 0; r < atoms; ++r) scales_to_tmem(tsfb + 4 * (j * atoms + r), sfb + r * 1024 + 512 * j);
+                const uint32_t tb0 = tsfb + (uint32_t)(first >> 5), tb1 = tb0 + 4u * (uint32_t)atoms;
+                scales_to_tmem(tsfa, sa);
+                for (int r = 0; r < atoms; ++r) scales_to_tmem(tsfb + 4 * r, sb + r * 64);
+                if (n64 > 2) {
+                    scales_to_tmem(tsfa + 4, sa + 32);
+                    for (int r = 0; r < atoms; ++r) scales_to_tmem(tsfb + 4 * (atoms + r), sb + r * 64 + 32);
                 }
-                for (int j = 0; j < n64; ++j)
-                    umma_mxf4(tmem, operand_desc(op + 32 * j), operand_desc(b + 32 * j), mx_instr_desc(a.bn, j & 1), tsfa + 4 * (j >> 1),
-                              tsfb + 4 * (j >> 1) * atoms + (first >> 5), (uint32_t)(i | j));
+                umma_mxf4(tmem, ad, bd, idesc0, tsfa, tb0, (uint32_t)i);
+                if (n64 > 1) umma_mxf4(tmem, ad + 2, bd + 2, idesc1, tsfa, tb0, 1);
+                if (n64 > 2) umma_mxf4(tmem, ad + 4, bd + 4, idesc0, tsfa + 4, tb1, 1);
+                if (n64 > 3) umma_mxf4(tmem, ad + 6, bd + 6, idesc1, tsfa + 4, tb1, 1);
                 umma_commit(&sh.empty[s]);
                 if (i + 1 == steps) umma_commit(&sh.done);
             }
             __syncwarp();
+            if (++s == a.stages) s = 0, phase ^= 1;
         }
         if (!ok) {   // the MMAs issued so far end before the tensor memory is given back
             if (elect_one()) umma_commit(&sh.done);
@@ -274,60 +349,54 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         fence_async_smem();
         mbar_arrive(&sh.ready);
     }
-    bool ok = true;
-    const int quarter = warp & 3, row = quarter * 32 + lane, o = ct * 128 + row;
-    if (warp >= 4) {
-        ok = mbar_wait(&sh.done, 0, abort, a.status, SBNN_ERR_TIMEOUT);
-        tc_fence_after_sync();
-    }
+    // All warps drain: two share a quarter of the lanes and halve the columns.
+    __syncwarp();
+    const bool ok = mbar_wait(&sh.done, 0, abort, a.status, SBNN_ERR_TIMEOUT);
+    tc_fence_after_sync();
+    const int row = (warp & 3) * 32 + lane, o = ct * 128 + row;
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const int middle = (a.bn / 8 + 1) / 2 * 8, c0 = warp < 4 ? 0 : middle, c1 = warp < 4 ? middle : a.bn;
+    Out<T> out;
+    out.mine = o < a.Cout;
+    out.y = static_cast<T*>(a.y) + (int64_t)n0 * a.ldy + o;
+    out.ldy = a.ldy;
+    out.bias = a.bias && out.mine ? __ldg(a.bias + o) : 0.f;
+    out.relu = a.relu;
+    out.pixels = min(a.bn, a.M - n0);
     if (a.split == 1) {
-        if (warp >= 4 && ok) {
-            const float bias = a.bias && o < a.Cout ? __ldg(a.bias + o) : 0.f;
-            for (int c0 = 0; c0 < a.bn; c0 += 16) {
-                uint32_t v[16];
-                tmem_ld(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c0, v);
-                tmem_ld_wait();
-#pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    const int64_t m = (int64_t)n0 + c0 + c;
-                    float f = __uint_as_float(v[c]) + bias;
-                    if (a.relu) f = fmaxf(f, 0.f);
-                    if (c0 + c < a.bn && m < a.M && o < a.Cout) store_any(a, m, o, f);
-                }
-            }
-        }
+        if (ok) drain(out, lanes, c0, c1);
     } else {
-        // every CTA of the cluster is done with its stages: their memory takes the sums that the others send
-        __syncwarp();
+        // Every CTA of the cluster is done with its stages: their memory takes the sums that the others send, four pixels of a
+        // channel at a time.  CTA r finishes pixels [r * width, (r + 1) * width).
         cluster_sync();
-        const int width = (a.bn + a.split - 1) / a.split;
-        float* const exchange = reinterpret_cast<float*>(base);
-        if (warp >= 4 && ok) {
-            const uint32_t ex = smem_u32(exchange);
-            for (int c0 = 0; c0 < a.bn; c0 += 16) {
-                uint32_t v[16];
-                tmem_ld(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c0, v);
+        const int width = exchange_width(a.bn, a.split);
+        const float4* const exchange = reinterpret_cast<const float4*>(base);
+        if (ok) {
+            const uint32_t ex = smem_u32(base);
+            int owner = c0 / width, first_of_owner = owner * width;
+            for (int c = c0; c < c1; c += 8) {
+                uint32_t v[8];
+                tmem_ld(lanes + (uint32_t)c, v);
                 tmem_ld_wait();
 #pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    const int col = c0 + c, owner = col / width;
-                    if (col < a.bn && n0 + col < a.M)
-                        store_remote(ex + (uint32_t)((rank * width + col - owner * width) * 128 + row) * 4u, (uint32_t)owner, __uint_as_float(v[c]));
+                for (int h = 0; h < 8; h += 4) {
+                    if (c + h >= first_of_owner + width) ++owner, first_of_owner += width;
+                    const int slot = (rank * width + c + h - first_of_owner) / 4 * 128 + row;
+                    if (c + h < out.pixels) store_remote(remote_address(ex + (uint32_t)slot * 16u, owner), v[h], v[h + 1], v[h + 2], v[h + 3]);
                 }
             }
         }
         __syncwarp();
         cluster_sync();
-        if (warp >= 4 && ok) {
-            const float bias = a.bias && o < a.Cout ? __ldg(a.bias + o) : 0.f;
-            for (int c = 0; c < width; ++c) {
-                const int col = rank * width + c;
-                if (col >= a.bn || n0 + col >= a.M) break;
-                float f = 0.f;
-                for (int r = 0; r < a.split; ++r) f += exchange[(r * width + c) * 128 + row];
-                f += bias;
-                if (a.relu) f = fmaxf(f, 0.f);
-                if (o < a.Cout) store_any(a, n0 + col, o, f);
+        if (ok) {
+            for (int c = warp < 4 ? 0 : 4; c < width && rank * width + c < out.pixels; c += 8) {
+                float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int r = 0; r < a.split; ++r) {
+                    const float4 g = exchange[(r * width + c) / 4 * 128 + row];
+                    f.x += g.x, f.y += g.y, f.z += g.z, f.w += g.w;
+                }
+                const uint32_t v[4] = {__float_as_uint(f.x), __float_as_uint(f.y), __float_as_uint(f.z), __float_as_uint(f.w)};
+                out.put(rank * width + c, v);
             }
         }
     }
@@ -382,9 +451,12 @@ sbnn_status launch(const Args& given, const Plan& p, const uint8_t* w_codes, con
     if ((r = encode_tiled_map(&wmap, w_codes, 2, 2, wdims, strides, wbox, 128)) != SBNN_OK) return r;
     if (p.fused) xmap = wmap;
     else if ((r = encode_tiled_map(&xmap, x_codes, 2, 2, xdims, strides, xbox, 128)) != SBNN_OK) return r;
-    auto* const kernel = p.fused ? conv_mxfp4_kernel<true> : conv_mxfp4_kernel<false>;
+    auto* const kernel = a.y_type == SBNN_F32   ? (p.fused ? conv_mxfp4_kernel<true, float> : conv_mxfp4_kernel<false, float>)
+                         : a.y_type == SBNN_F16 ? (p.fused ? conv_mxfp4_kernel<true, __half> : conv_mxfp4_kernel<false, __half>)
+                                                : (p.fused ? conv_mxfp4_kernel<true, __nv_bfloat16> : conv_mxfp4_kernel<false, __nv_bfloat16>);
     if ((r = set_max_dyn_smem(reinterpret_cast<const void*>(kernel), kMaxSmem)) != SBNN_OK) return r;
     const size_t smem = (size_t)layout_of(a.bn, a.stages, (a.steps + a.split - 1) / a.split, p.fused).total;
+    ChainedLaunchScope chained;   // the set-up overlaps the end of the launch before
     SBNN_CUDA_TRY(launch_kernel_cluster(kernel, dim3((unsigned)ctas), dim3(kThreads), smem, st, (unsigned)a.split, wmap, xmap, a));
     return SBNN_OK;
 }
@@ -455,5 +527,6 @@ extern "C" sbnn_status sbnn_conv1x1_mxfp4(const uint8_t* w_codes_dev, const uint
     uint8_t* const xc = static_cast<uint8_t*>(workspace_dev);
     a.x_scales = xc + codes;
     if ((r = mxfp4_quantize_launch(x_dev, x_type, ldx, xc, xc + codes, M, Cin, st)) != SBNN_OK) return r;
+    a.early = 1;
     return launch(a, p, w_codes_dev, xc, st);
 }

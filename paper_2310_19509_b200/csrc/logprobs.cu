@@ -303,6 +303,7 @@ logprobs_kernel(const Params p) {
     constexpr int TEAMS = NT == 32 ? 8 : 1, N = Vec<T>::N, U = 4;
     __shared__ Team<NT> teams[TEAMS];
     grid_dependency_wait();
+    grid_dependency_release();
     Team<NT>& t = teams[threadIdx.x / NT];
     const int id = threadIdx.x % NT, lane = id & 31, warp = id >> 5;
     const int64_t r = NT == 32 ? (int64_t)blockIdx.x * TEAMS + threadIdx.x / NT : blockIdx.x / p.parts;
@@ -394,6 +395,7 @@ sbnn_status launch_as(const Params& given, cudaStream_t st) {
     const int64_t bytes = (int64_t)p.classes * sizeof(T);
     const int sms = device_sms();
     p.parts = 1;
+    ChainedLaunchScope chained;
     if (bytes <= 4096 && p.rows >= 8 * sms) {
         SBNN_CUDA_TRY(launch_kernel(logprobs_kernel<T, 32>, dim3((unsigned)((p.rows + 7ll) / 8)), dim3(256), 0, st, p));
         return SBNN_OK;

@@ -21,6 +21,7 @@ __global__ void __launch_bounds__(256)
 quantize_kernel(const T* __restrict__ x, int64_t ldx, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, int M, int K, int ktiles) {
     __shared__ uint32_t tile[kRows];   // [row % 32][row / 32]: four scale bytes each
     grid_dependency_wait();
+    grid_dependency_release();   // behind the wait: what starts now knows all launches before this one to be done
     const int lane = threadIdx.x & 31, half = lane >> 4, part = lane & 15, warp = threadIdx.x >> 5;
     const int kt = blockIdx.x % ktiles;
     const int64_t row0 = (int64_t)(blockIdx.x / ktiles) * kRows;
@@ -65,6 +66,7 @@ template <class T, bool VEC>
 __global__ void __launch_bounds__(256)
 dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ y, int64_t ldy, int M, int K, int ktiles) {
     grid_dependency_wait();
+    grid_dependency_release();   // behind the wait: what starts now knows all launches before this one to be done
     const int lane = threadIdx.x & 31, half = lane >> 4, part = lane & 15, warp = threadIdx.x >> 5;
     const int kt = blockIdx.x % ktiles;
     const int64_t row0 = (int64_t)(blockIdx.x / ktiles) * kRows;
@@ -125,6 +127,7 @@ sbnn_status quantize_as(const void* x, int64_t ldx, uint8_t* codes, uint8_t* sca
     const sbnn_status r = grid_of(M, K, &blocks);
     if (r != SBNN_OK) return r;
     auto* const kernel = whole_vectors(x, ldx, K, sizeof(T)) ? quantize_kernel<T, true> : quantize_kernel<T, false>;
+    ChainedLaunchScope chained;
     SBNN_CUDA_TRY(launch_kernel(kernel, dim3(blocks), dim3(256), 0, st, static_cast<const T*>(x), ldx, codes, scales, M, K, mx_ktiles(K)));
     return SBNN_OK;
 }
@@ -134,6 +137,7 @@ sbnn_status dequantize_as(const uint8_t* codes, const uint8_t* scales, void* y, 
     const sbnn_status r = grid_of(M, K, &blocks);
     if (r != SBNN_OK) return r;
     auto* const kernel = whole_vectors(y, ldy, K, sizeof(T)) ? dequantize_kernel<T, true> : dequantize_kernel<T, false>;
+    ChainedLaunchScope chained;
     SBNN_CUDA_TRY(launch_kernel(kernel, dim3(blocks), dim3(256), 0, st, codes, scales, static_cast<T*>(y), ldy, M, K, mx_ktiles(K)));
     return SBNN_OK;
 }
