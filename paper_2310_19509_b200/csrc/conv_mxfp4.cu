@@ -20,6 +20,7 @@
 
 #include "common.h"
 #include "mxfp4.cuh"
+#include "mxfp4_mma.cuh"
 #include "pipeline.cuh"
 #include "tcgen05.cuh"
 
@@ -30,7 +31,6 @@ sbnn_status mxfp4_quantize_launch(const void* x, int x_type, int64_t ldx, uint8_
 namespace {
 
 constexpr int kThreads = 256;       // warp 0 copies, warp 1 issues MMAs, warps 4-7 drain; warps 2-7 round activations (FUSED)
-constexpr int kStep = 256;          // channels of a pipeline step: 128 bytes of codes a row
 constexpr int kABytes = 128 * 128;  // the weights of a step
 constexpr int kMaxStages = 8;
 constexpr int kFusedPixels = SBNN_MXFP4_DIRECT_ROWS;
@@ -85,15 +85,6 @@ __host__ __device__ inline uint32_t tmem_columns(int bn, int stages) {
     return c;
 }
 
-// ---- block-scaled MMA ------------------------------------------------------------------------------
-// Instruction descriptor: e2m1 x e2m1 -> fp32, both K-major, M = 128, N = n, scales are powers of two (ue8m0), two a row and
-// MMA; `half` says which two of the four bytes of a scale word.
-__device__ __forceinline__ uint32_t mx_instr_desc(int n, int half) {
-    return ((uint32_t)(2 * half) << 4)         // B: scale factor id 0 or 2
-           | (1u << 7) | (1u << 10)            // A and B: e2m1
-           | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(128 >> 7) << 27)
-           | ((uint32_t)(2 * half) << 29);     // A: scale factor id
-}
 __device__ __forceinline__ void umma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -102,33 +93,9 @@ __device__ __forceinline__ void umma_mxf4(uint32_t d, uint64_t a, uint64_t b, ui
         ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
         : "memory");
 }
-// Descriptor of 512 bytes of scales: 32 rows of 16 bytes, linear.
-__device__ __forceinline__ uint64_t scale_desc(uint32_t smem) {
-    uint64_t d = (uint64_t)((smem & 0x3FFFFu) >> 4);
-    d |= (uint64_t)1 << 16;            // leading byte offset: not used, rows are 16 bytes
-    d |= (uint64_t)(128 >> 4) << 32;   // groups of 8 rows are 128 bytes apart
-    d |= (uint64_t)1 << 46;            // descriptor version; no swizzle
-    return d;
-}
-// Those into 4 columns, the same in each quarter of the lanes.
+// 512 bytes of scales into 4 columns, the same in each quarter of the lanes.
 __device__ __forceinline__ void scales_to_tmem(uint32_t tmem, uint64_t d) {
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(d) : "memory");
-}
-
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-// The address that `addr` has in the shared memory of CTA `rank` of the cluster.
-__device__ __forceinline__ uint32_t remote_address(uint32_t addr, int rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
 }
 __device__ __forceinline__ void store_remote(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -307,7 +274,7 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         // than its MMAs (one token, 8192 -> 16384: 25.1 us, like this 17.6).
         const uint64_t a0 = operand_desc(smem_u32(base)), b0 = operand_desc(FUSED ? smem_u32(resident) : smem_u32(base) + (uint32_t)l.a);
         const uint64_t sfa0 = scale_desc(smem_u32(scales)), sfb0 = scale_desc(FUSED ? smem_u32(resident_sf) : smem_u32(scales) + (uint32_t)l.sfa);
-        const uint32_t idesc0 = mx_instr_desc(a.bn, 0), idesc1 = mx_instr_desc(a.bn, 1);
+        const uint32_t idesc0 = mx_instr_desc(128, a.bn, 0), idesc1 = mx_instr_desc(128, a.bn, 1);
         int s = 0;
         uint32_t phase = 0;
         for (int i = 0; ok && i < steps; ++i) {
@@ -408,23 +375,42 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
 // ---- host ------------------------------------------------------------------------------------------
 struct Plan {
     int bn, split, stages;
-    bool fused;
+    bool fused, pair;
 };
 
-// Tiles of 256 pixels where they fill the SMs, else of 128 or 64, else (up to 32 pixels) one tile as wide as the pixels; the
-// steps of tiles that are still fewer than half the SMs are shared, two steps a CTA at least.
-Plan plan_for(int64_t M, int Cout, int K, bool raw) {
+// Microseconds that a launch of this kernel takes, and one of the kernel of CTA pairs, fitted to what they were measured at (their
+// rounding apart): a CTA starts, fills its pipeline and drains in 2.4 + 0.024 BN, a step brings in 17 KB of weights and 136 bytes a
+// pixel at 45 bytes a clock and SM, sharing a tile costs the exchange.  300 pixels 4096 -> 4096: tiles of 64 in two waves 18.0 (model
+// 18.0), of pairs 10.4 (11.9); 588, 1024 -> 516 fp32: tiles of 64 shared by two 5.8 (5.5), pairs 8.5 (7.9); 2048, 256 -> 4096:
+// tiles of 256 16.7 (18.0), pairs 11.3 (10.3); 8192, 8192 -> 8192: 327 (316) and 192 (168).
+double tile_us(int bn) { return 2.4 + 0.024 * bn; }
+double step_us(int bn) { return 0.215 + 0.00168 * bn; }
+double single_us(int64_t tiles, int steps, int bn, int split, int sms) {
+    const int64_t waves = (tiles * split + sms - 1) / sms;
+    return (double)waves * (tile_us(bn) + (double)((steps + split - 1) / split) * step_us(bn)) + (split > 1 ? 1.0 : 0.0);
+}
+double pair_us(int64_t M, int Cout, int steps, int y_bytes, int sms) {
+    const int64_t tiles = ((M + 255) / 256) * (((int64_t)Cout + 255) / 256), waves = (tiles + sms / 2 - 1) / (sms / 2);
+    const double sums = 0.36 * steps;   // 256 channels of a tile; its epilogue takes 3.4 (fp32 5.2), unless the sums of the next do
+    return 6.5 + sums + (double)(waves - 1) * std::max(sums, y_bytes == 4 ? 5.2 : 3.4);
+}
+
+// Up to 32 pixels: one tile as wide as the pixels.  Else the width and the number of CTAs that share a tile's steps, all
+// resident at the same time, that take least by the model, or the kernel of pairs.
+Plan plan_for(int64_t M, int Cout, int K, bool raw, int y_bytes) {
     const int sms = device_sms(), ctiles = (Cout + 127) / 128, steps = (K + kStep - 1) / kStep;
-    Plan p;
-    p.bn = 64;
-    if (M <= kFusedPixels) p.bn = (int)(M + 7) / 8 * 8;
-    else if (ctiles * ((M + 255) / 256) >= sms) p.bn = 256;
-    else if (ctiles * ((M + 127) / 128) >= sms) p.bn = 128;
-    const int64_t tiles = ctiles * ((M + p.bn - 1) / p.bn);
-    p.split = 1;
-    while (p.split < 8 && tiles * (p.split + 1) <= sms && steps >= 2 * (p.split + 1)) ++p.split;
-    p.fused = false;
-    if (raw && M <= kFusedPixels) {
+    Plan p = {};
+    double best = 1e30;
+    const int few = M <= kFusedPixels ? (int)(M + 7) / 8 * 8 : 0;
+    for (int bn = few ? few : 64; bn <= (few ? few : 256); bn *= 2) {
+        const int64_t tiles = ctiles * ((M + bn - 1) / bn);
+        for (int split = 1; split <= 8 && split <= steps && (split == 1 || tiles * split <= sms); ++split) {
+            const double us = single_us(tiles, steps, bn, split, sms);
+            if (us < best) best = us, p.bn = bn, p.split = split;
+        }
+    }
+    p.pair = !few && pair_us(M, Cout, steps, y_bytes, sms) < best;
+    if (raw && few) {
         while (p.split < 8 && layout_of(p.bn, 4, (steps + p.split - 1) / p.split, true).total > kMaxSmem) ++p.split;
         p.fused = layout_of(p.bn, 4, (steps + p.split - 1) / p.split, true).total <= kMaxSmem;
     }
@@ -434,6 +420,11 @@ Plan plan_for(int64_t M, int Cout, int K, bool raw) {
 }
 
 sbnn_status launch(const Args& given, const Plan& p, const uint8_t* w_codes, const uint8_t* x_codes, cudaStream_t st) {
+    if (p.pair) {
+        const MxProduct q = {w_codes, given.w_scales, x_codes, given.x_scales, given.bias, given.y, given.ldy, given.y_type, given.M, given.Cout, given.K,
+                             given.relu};
+        return conv_mxfp4_pair(q, st);
+    }
     Args a = given;
     sbnn_status r = async_status_word(&a.status);
     if (r != SBNN_OK) return r;
@@ -491,7 +482,7 @@ extern "C" sbnn_status sbnn_conv1x1_mxfp4_q(const uint8_t* w_codes_dev, const ui
     Args a = {};
     a.w_scales = w_scales_dev, a.x_scales = x_scales_dev, a.bias = bias_dev, a.y = y_dev, a.ldy = ldy, a.y_type = y_type;
     a.M = M, a.Cout = Cout, a.K = Cin, a.relu = flags & SBNN_RELU;
-    return launch(a, plan_for(M, Cout, Cin, false), w_codes_dev, x_codes_dev, static_cast<cudaStream_t>(cuda_stream));
+    return launch(a, plan_for(M, Cout, Cin, false, y_type == SBNN_F32 ? 4 : 2), w_codes_dev, x_codes_dev, static_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" sbnn_status sbnn_conv1x1_mxfp4(const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, const float* bias_dev, const void* x_dev,
@@ -517,7 +508,7 @@ extern "C" sbnn_status sbnn_conv1x1_mxfp4(const uint8_t* w_codes_dev, const uint
     Args a = {};
     a.w_scales = w_scales_dev, a.bias = bias_dev, a.y = y_dev, a.ldy = ldy, a.y_type = y_type;
     a.M = M, a.Cout = Cout, a.K = Cin, a.relu = flags & SBNN_RELU;
-    const Plan p = plan_for(M, Cout, Cin, true);
+    const Plan p = plan_for(M, Cout, Cin, true, y_type == SBNN_F32 ? 4 : 2);
     if (p.fused) {
         a.x = x_dev, a.ldx = ldx, a.x_type = x_type;
         a.vec = ldx * (x_type == SBNN_F32 ? 4 : 2) % 16 == 0;

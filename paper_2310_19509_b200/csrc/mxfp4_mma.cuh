@@ -1,0 +1,56 @@
+// What the two kernels that multiply microscaled 4-bit operands share: descriptors of block-scaled MMAs, clusters.
+#pragma once
+
+#include <stdint.h>
+
+#include "pipeline.cuh"
+
+namespace sbnn {
+
+constexpr int kStep = 256;   // channels of a pipeline step: 128 bytes of codes a row
+
+// Arguments of a product whose activations are rounded already.
+struct MxProduct {
+    const uint8_t *w_codes, *w_scales, *x_codes, *x_scales;
+    const float* bias;
+    void* y;
+    int64_t ldy;
+    int y_type, M, Cout, K, relu;
+};
+// conv_mxfp4_pair.cu: pairs of CTAs on 256 x 256 tiles.
+sbnn_status conv_mxfp4_pair(const MxProduct& p, cudaStream_t st);
+
+// Instruction descriptor: e2m1 x e2m1 -> fp32, both K-major, m x n, scales are powers of two (ue8m0), two a row and MMA;
+// `half` says which two of the four bytes of a scale word.
+__device__ __forceinline__ uint32_t mx_instr_desc(int m, int n, int half) {
+    return ((uint32_t)(2 * half) << 4)         // B: scale factor id 0 or 2
+           | (1u << 7) | (1u << 10)            // A and B: e2m1
+           | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 7) << 27)
+           | ((uint32_t)(2 * half) << 29);     // A: scale factor id
+}
+// Descriptor of 512 bytes of scales in shared memory: 32 rows of 16 bytes, linear.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t smem) {
+    uint64_t d = (uint64_t)((smem & 0x3FFFFu) >> 4);
+    d |= (uint64_t)1 << 16;            // leading byte offset: not used, rows are 16 bytes
+    d |= (uint64_t)(128 >> 4) << 32;   // groups of 8 rows are 128 bytes apart
+    d |= (uint64_t)1 << 46;            // descriptor version; no swizzle
+    return d;
+}
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// The address that `addr` has in the shared memory of CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t remote_address(uint32_t addr, int rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+
+}  // namespace sbnn
