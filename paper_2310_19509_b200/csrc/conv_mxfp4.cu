@@ -268,8 +268,8 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 for (int i = max(0, issued - a.stages); i < issued; ++i) land(&sh.full[i % a.stages], (i / a.stages) & 1);
         }
     } else if (warp == 1) {
-        bool ok = true;
-        if (FUSED) ok = mbar_wait(&sh.ready, 0, abort, a.status, SBNN_ERR_TIMEOUT);
+        bool ok = !FUSED || __all_sync(~0u, mbar_wait(&sh.ready, 0, abort, a.status, SBNN_ERR_TIMEOUT));
+        const uint32_t tmem = __shfl_sync(~0u, sh.tmem, 0), tmem_sf = tmem + (uint32_t)((a.bn + 31) / 32 * 32);   // in uniform registers
         // Everything that the issuing lane needs is kept by addition: divisions and rebuilt descriptors of a step took longer
         // than its MMAs (one token, 8192 -> 16384: 25.1 us, like this 17.6).
         const uint64_t a0 = operand_desc(smem_u32(base)), b0 = operand_desc(FUSED ? smem_u32(resident) : smem_u32(base) + (uint32_t)l.a);
@@ -278,7 +278,7 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         int s = 0;
         uint32_t phase = 0;
         for (int i = 0; ok && i < steps; ++i) {
-            if (!(ok = mbar_wait(&sh.full[s], phase, abort, a.status, SBNN_ERR_TIMEOUT))) break;
+            if (!(ok = __all_sync(~0u, mbar_wait(&sh.full[s], phase, abort, a.status, SBNN_ERR_TIMEOUT)))) break;
             tc_fence_after_sync();
             const uint32_t tsfa = tmem_sf + (uint32_t)s * sf_cols, tsfb = tsfa + 8;
             const uint64_t ad = a0 + (uint32_t)(s * (op_stage >> 4)), bd = b0 + (uint32_t)(FUSED ? i * (l.b >> 4) : s * (op_stage >> 4));

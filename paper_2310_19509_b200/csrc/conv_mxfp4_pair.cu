@@ -193,15 +193,16 @@ conv_mxfp4_pair_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_co
     } else if (warp == 1 && rank == 0) {
         const uint64_t a0 = operand_desc(smem_u32(base)), b0 = operand_desc(smem_u32(base + kOperand)), f0 = scale_desc(smem_u32(scales));
         const uint32_t idesc0 = mx_instr_desc(256, 256, 0), idesc1 = mx_instr_desc(256, 256, 1);
+        const uint32_t tmem = __shfl_sync(~0u, sh.tmem, 0);   // in a uniform register
         int s = 0, done = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (int t = pair; ok && t < tiles; t += pairs, ++done) {
-            if (done && !(ok = pair_wait(&sh.freed, (done - 1) & 1, abort, a.status))) break;
+            if (done && !(ok = __all_sync(~0u, pair_wait(&sh.freed, (done - 1) & 1, abort, a.status)))) break;
             tc_fence_after_sync();
             const uint32_t d = tmem + (done & 1 ? kSecond : 0);
             for (int i = 0; i < steps; ++i) {
-                if (!(ok = pair_wait(&sh.full[s], phase, abort, a.status))) break;
+                if (!(ok = __all_sync(~0u, pair_wait(&sh.full[s], phase, abort, a.status)))) break;
                 tc_fence_after_sync();
                 const uint32_t sfa = tmem + kScales + 24 * s, sfb = sfa + 8;
                 const uint64_t ad = a0 + (uint32_t)(s * (2 * kOperand >> 4)), bd = b0 + (uint32_t)(s * (2 * kOperand >> 4)), fd = f0 + (uint32_t)(s * 192);
