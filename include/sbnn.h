@@ -485,13 +485,14 @@ SBNN_API sbnn_status sbnn_mxfp4_dequantize(const uint8_t* codes_dev, const uint8
  *   flags                      SBNN_RELU or 0
  *   workspace_dev              device memory for the rounded activations, the two sizes of sbnn_mxfp4_bytes(M, Cin) added; of
  *                              the caller, so that calls in flight at the same time, and graphs, can have their own.  Not used,
- *                              and may be NULL, for M <= SBNN_MXFP4_DIRECT_ROWS.
+ *                              and may be NULL, for M <= SBNN_MXFP4_DIRECT_ROWS and Cin <= SBNN_MXFP4_DIRECT_CHANNELS.
  * sbnn_conv1x1_mxfp4_q takes activations that are in 4-bit form already (several layers on the same activations round them once).
  * A pixel's result does not depend on other pixels' values; the order of its sums depends on M, Cin and Cout alone.  A NaN block
  * makes every output that it meets NaN (0 after ReLU, as max(NaN, 0) is everywhere in this library).
  * Nothing is allocated or kept between calls.
  */
 #define SBNN_MXFP4_DIRECT_ROWS 32
+#define SBNN_MXFP4_DIRECT_CHANNELS 65536
 SBNN_API sbnn_status sbnn_conv1x1_mxfp4(const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, const float* bias_dev,
                                         const void* x_dev, int x_type, int64_t ldx, void* y_dev, int y_type, int64_t ldy,
                                         int M, int Cin, int Cout, int flags, void* workspace_dev, int64_t workspace_bytes,

@@ -34,7 +34,7 @@ constexpr int kThreads = 256;       // warp 0 copies, warp 1 issues MMAs, warps 
 constexpr int kABytes = 128 * 128;  // the weights of a step
 constexpr int kMaxStages = 8;
 constexpr int kFusedPixels = SBNN_MXFP4_DIRECT_ROWS;
-constexpr int kMaxSmem = 227 * 1024;
+constexpr int kMaxSmem = 227 * 1024, kHalfSmem = 113 * 1024;   // of one CTA, of two on an SM
 
 struct Args {
     const uint8_t *w_scales, *x_scales;
@@ -110,35 +110,51 @@ __device__ __forceinline__ void land(uint64_t* bar, uint32_t parity) {
 }
 
 // ---- activations of a FUSED call: rounded by the CTA for the steps that it sums -------------------------
+// A thread takes whole blocks, U of them at a time: 4 U loads are on their way before the first is used.  (Four lanes a block, 8
+// channels each, read whole lines but need more rounds: 13 pixels 8192 -> 8192 14.4 us and one token 4096 -> 16384 10.6, like this
+// 13.2 and 9.6.)
+template <class T, bool VEC, int U>
+__device__ __forceinline__ void round_blocks(const Args& a, uint8_t* b, uint8_t* sfb, int b_bytes, int sfb_bytes, int step0, int blocks, int i, int nt) {
+    Eight<T> e[U][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int row = (i + u * nt) / blocks, blk = (i + u * nt) - row * blocks, k = (step0 * 8 + blk) * 32, n = a.K - k;
+        const T* p = static_cast<const T*>(a.x) + row * a.ldx + k;
+        if (VEC && n >= 32) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) load8<true>(e[u][q], p + 8 * q, 8);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[u][q].v[j] = 8 * q + j < n ? __ldg(p + 8 * q + j) : from_float<T>(0.f);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int row = (i + u * nt) / blocks, blk = (i + u * nt) - row * blocks, s = blk >> 3, c = blk & 7;
+        uint32_t m = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) m = max(m, largest_bits(e[u][q]));
+        const uint32_t byte = mx_scale_byte(m);
+        *reinterpret_cast<uint4*>(b + s * b_bytes + row * 128 + ((c ^ (row & 7)) << 4)) =
+            make_uint4(encode8(e[u][0], byte), encode8(e[u][1], byte), encode8(e[u][2], byte), encode8(e[u][3], byte));
+        sfb[s * sfb_bytes + (c >> 2) * 512 + row * 16 + (c & 3)] = (uint8_t)byte;   // row < 32
+    }
+}
 template <class T, bool VEC>
-__device__ __forceinline__ void round_block(const T* p, int n, uint4& codes, uint32_t& byte) {
-    Eight<T> e[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) load8<VEC>(e[i], p + 8 * i, n - 8 * i);
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m = max(m, largest_bits(e[i]));
-    byte = mx_scale_byte(m);
-    codes = make_uint4(encode8(e[0], byte), encode8(e[1], byte), encode8(e[2], byte), encode8(e[3], byte));
+__device__ __forceinline__ void round_pixels_as(const Args& a, uint8_t* b, uint8_t* sfb, int b_bytes, int sfb_bytes, int step0, int steps, int t, int nt) {
+    const int blocks = steps * 8, total = a.M * blocks;
+    int i = t;
+    if (VEC && sizeof(T) == 2)
+        for (; i + nt < total; i += 2 * nt) round_blocks<T, VEC, 2>(a, b, sfb, b_bytes, sfb_bytes, step0, blocks, i, nt);
+#pragma unroll 1
+    for (; i < total; i += nt) round_blocks<T, VEC, 1>(a, b, sfb, b_bytes, sfb_bytes, step0, blocks, i, nt);
 }
 template <class T>
 __device__ __forceinline__ void round_pixels(const Args& a, uint8_t* b, uint8_t* sfb, int b_bytes, int sfb_bytes, int step0, int steps, int t, int nt) {
-    const int blocks = steps * 8;
-    const T* x = static_cast<const T*>(a.x);
-    for (int i = t; i < a.M * blocks; i += nt) {
-        const int row = i / blocks, blk = i % blocks, s = blk >> 3, c = blk & 7, k = (step0 * 8 + blk) * 32, n = a.K - k;
-        uint4 codes = make_uint4(0, 0, 0, 0);
-        uint32_t byte = 0;
-        if (n > 0) {
-            const T* p = x + row * a.ldx + k;
-            if (a.vec && n >= 32)
-                round_block<T, true>(p, 32, codes, byte);
-            else
-                round_block<T, false>(p, n, codes, byte);
-        }
-        *reinterpret_cast<uint4*>(b + s * b_bytes + row * 128 + ((c ^ (row & 7)) << 4)) = codes;
-        sfb[s * sfb_bytes + (c >> 2) * 512 + row * 16 + (c & 3)] = (uint8_t)byte;   // row < 32
-    }
+    if (a.vec) round_pixels_as<T, true>(a, b, sfb, b_bytes, sfb_bytes, step0, steps, t, nt);
+    else round_pixels_as<T, false>(a, b, sfb, b_bytes, sfb_bytes, step0, steps, t, nt);
 }
 
 // ---- epilogue: one output channel a lane ---------------------------------------------------------------
@@ -395,27 +411,51 @@ double pair_us(int64_t M, int Cout, int steps, int y_bytes, int sms) {
     return 6.5 + sums + (double)(waves - 1) * std::max(sums, y_bytes == 4 ? 5.2 : 3.4);
 }
 
-// Up to 32 pixels: one tile as wide as the pixels.  Else the width and the number of CTAs that share a tile's steps, all
-// resident at the same time, that take least by the model, or the kernel of pairs.
+// The same for up to 32 pixels (one tile as wide as they are), where a step is bound by the chain of its copies and MMAs, 0.3 us, or
+// 0.55 with two CTAs on an SM, and sharing a tile by the exchange; `pixels`: of those that the CTAs round themselves.  One token 8192 ->
+// 8192 shared by 2 10.4, by 4 9.7; 4096 -> 4096 by 2, 4, 8 6.3, 5.5, 6.1; 1024 -> 1000 by 1, 2, 4 3.6, 4.2, 4.1.
+double few_us(int64_t tiles, int steps, int split, int pixels, int sms) {
+    const int own = (steps + split - 1) / split, rounds = (pixels * own * 32 + 1535) / 1536;
+    return 2.6 + (split > 1 ? 0.6 + 0.12 * split : 0.0) + own * (tiles * split > sms ? 0.55 : 0.3) * std::max(1.0, (double)(tiles * split) / (2 * sms)) +
+           0.55 * rounds;
+}
+
+// The width of a tile and the number of CTAs that share its steps, all resident at the same time, that take least by the model, or
+// the kernel of pairs.
 Plan plan_for(int64_t M, int Cout, int K, bool raw, int y_bytes) {
     const int sms = device_sms(), ctiles = (Cout + 127) / 128, steps = (K + kStep - 1) / kStep;
     Plan p = {};
     double best = 1e30;
-    const int few = M <= kFusedPixels ? (int)(M + 7) / 8 * 8 : 0;
-    for (int bn = few ? few : 64; bn <= (few ? few : 256); bn *= 2) {
+    if (M <= kFusedPixels) {
+        // One plan for both entry points, as if the CTAs rounded the activations, so that their results are the same bits.  First
+        // what is resident at once; else any cluster that holds its share of the activations; else none does: rounded ahead.
+        p.bn = (int)(M + 7) / 8 * 8;
+        for (int pass = 0; pass < 3 && best == 1e30; ++pass) {
+            p.fused = raw && pass < 2;
+            for (int split = 1; split <= 8 && split <= steps && (pass || split == 1 || ctiles * split <= 2 * sms); ++split) {
+                const int own = (steps + split - 1) / split;
+                const bool two = ctiles * split > sms && !pass;
+                const auto stages_in = [&](bool fused) {
+                    int n = 6;
+                    while (n > 0 && layout_of(p.bn, n, own, fused).total > (two ? kHalfSmem : kMaxSmem)) --n;
+                    return n;
+                };
+                if (stages_in(pass < 2) < (two ? 4 : 2)) continue;
+                const double us = few_us(ctiles, steps, split, (int)M, sms);
+                if (us < best) best = us, p.split = split, p.stages = stages_in(p.fused);
+            }
+        }
+        return p;
+    }
+    for (int bn = 64; bn <= 256; bn *= 2) {
         const int64_t tiles = ctiles * ((M + bn - 1) / bn);
         for (int split = 1; split <= 8 && split <= steps && (split == 1 || tiles * split <= sms); ++split) {
             const double us = single_us(tiles, steps, bn, split, sms);
             if (us < best) best = us, p.bn = bn, p.split = split;
         }
     }
-    p.pair = !few && pair_us(M, Cout, steps, y_bytes, sms) < best;
-    if (raw && few) {
-        while (p.split < 8 && layout_of(p.bn, 4, (steps + p.split - 1) / p.split, true).total > kMaxSmem) ++p.split;
-        p.fused = layout_of(p.bn, 4, (steps + p.split - 1) / p.split, true).total <= kMaxSmem;
-    }
+    p.pair = pair_us(M, Cout, steps, y_bytes, sms) < best;
     p.stages = p.bn <= 128 ? 6 : 4;
-    while (p.stages > 2 && layout_of(p.bn, p.stages, (steps + p.split - 1) / p.split, p.fused).total > kMaxSmem) --p.stages;
     return p;
 }
 
@@ -514,7 +554,8 @@ extern "C" sbnn_status sbnn_conv1x1_mxfp4(const uint8_t* w_codes_dev, const uint
         a.vec = ldx * (x_type == SBNN_F32 ? 4 : 2) % 16 == 0;
         return launch(a, p, w_codes_dev, nullptr, st);
     }
-    if (M <= kFusedPixels) return fail(SBNN_ERR_UNSUPPORTED, "Cin=%d is too wide for so few pixels", Cin);
+    if (!workspace_dev || workspace_bytes < codes + scales || !aligned16(workspace_dev))
+        return fail(SBNN_ERR_NULL, "Cin=%d is too wide to be rounded without a workspace of %lld bytes", Cin, (long long)(codes + scales));
     uint8_t* const xc = static_cast<uint8_t*>(workspace_dev);
     a.x_scales = xc + codes;
     if ((r = mxfp4_quantize_launch(x_dev, x_type, ldx, xc, xc + codes, M, Cin, st)) != SBNN_OK) return r;

@@ -154,10 +154,32 @@ def check_layer(m, k, n, dtype, seed=0, **kw):
 
 
 @pytest.mark.parametrize("m,k,n", [(1, 32, 128), (1, 64, 1), (1, 1, 5), (8, 256, 128), (3, 96, 130), (1, 1024, 1000), (13, 700, 300), (32, 512, 257),
-                                   (17, 4096, 64), (2, 8200, 130), (32, 16384, 16), (1, 40000, 40)])
+                                   (17, 4096, 64), (2, 8200, 130), (32, 16384, 16), (1, 40000, 40), (32, 65536, 20)])
 @pytest.mark.parametrize("pre", [False, True])
 def test_few_pixels(m, k, n, pre):
     check_layer(m, k, n, "f32", m + k + n, pre=pre)
+
+
+@pytest.mark.parametrize("m,k,n", [(32, 10240, 19300), (9, 2000, 40001), (700, 512, 33000)])
+def test_many_channels_sampled(m, k, n):
+    """Weights that are drawn as codes and scales; some channels of each end and between."""
+    g = torch.Generator(device="cuda").manual_seed(k)
+    codes = torch.randint(256, (n, 16 * O.blocks_of(k)), generator=g, device="cuda", dtype=torch.uint8)
+    if k % 32:
+        codes[:, k // 2:] = 0
+    scales = torch.randint(118, 124, (sbnn.mxfp4_bytes(n, k)[1],), generator=g, device="cuda", dtype=torch.uint8)
+    x = activations(m, k, "bf16", 18)
+    y = torch.empty((m, n), device="cuda")
+    work = torch.empty((sum(sbnn.mxfp4_bytes(m, k)),), dtype=torch.uint8, device="cuda") if m > 32 else None
+    sbnn.conv1x1_mxfp4(codes, scales, None, x.cuda(), k, y, n, m, k, n, 0, work)
+    sbnn.get_async_status()
+    rows = torch.cat((torch.arange(130), torch.randint(n, (100,), generator=torch.Generator().manual_seed(1)), torch.arange(n - 130, n)))
+    off = O.scale_offsets(n, k)[rows]
+    wv = O.values(codes[rows.cuda()].cpu().numpy(), scales.cpu().numpy()[off], k)
+    xv = O.values(*O.quantize(x.double().numpy()), k)
+    ref, s = O.conv1x1(xv, wv, None, False)
+    got = y[:, rows.cuda()].cpu().double().numpy()
+    assert np.all(np.abs(got - ref) <= bound(k, s, ref, "f32"))
 
 
 @pytest.mark.parametrize("m,k,n", [(33, 64, 128), (64, 256, 128), (65, 300, 516), (128, 1024, 128), (129, 128, 1000), (196, 517, 516), (500, 2048, 256),
