@@ -1,12 +1,12 @@
 // Log probabilities of given classes, entropy and the most probable classes of rows of logits.
 //
-//   lse = m + log s,  m = max x,  s = sum e^(x - m);   log p(c) = x_c - lse
-//   entropy = -sum p log p = log s - u / s,  u = sum e^(x - m) (x - m)
+//   t = (x - m) log2 e,  m = max x,  s = sum 2^t,  u = sum 2^t t;   log p(c) = (t_c - log2 s) ln 2
+//   entropy = -sum p log p = (log2 s - u / s) ln 2
 //
 // Bound: memory; the logits are read once.  Every thread keeps m, s and u of its own share; where that fits its registers
 // (RES) it is held there and m is known before the first exponential, else s and u are brought down whenever a larger m comes
-// (e^d, d = old - new: s' = e^d s, u' = e^d (u + d s)).  Shares are joined the same way.  Exponentials, sums and products are
-// packed in pairs: 5.5 instructions a bf16 logit instead of 8.5.
+// (2^d, d the old one's t: s' = 2^d s, u' = 2^d (u + d s)).  Shares are joined the same way.  Exponentials, sums and products are
+// packed in pairs.
 //
 // The k most probable classes come out of the same pass: the threads of a team are dealt to groups, and the k-th largest of
 // the groups' maxima is a bound that at least k classes reach and few more.  Only threads whose own maximum reaches it look
@@ -28,14 +28,13 @@ namespace {
 constexpr int kMaxTop = SBNN_LOGPROBS_MAX_TOP;
 constexpr int kHeld = 8;        // 16-byte vectors of a row that a thread holds (RES)
 constexpr float kLog2E = 1.4426950408889634f;
-constexpr float kFar = -1e30f;   // differences below it count as it: e^kFar = 0, and 0 * kFar is 0, which 0 * -inf is not
+constexpr float kFar = -1e30f;   // a t below it counts as it: 2^kFar = 0, and 0 * kFar is 0, which 0 * -inf is not
 
 __device__ __forceinline__ float exp2_of(float t) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
     return r;
 }
-__device__ __forceinline__ float exp_of(float d) { return exp2_of(d * kLog2E); }
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -61,13 +60,30 @@ __device__ __forceinline__ uint32_t key_of(float v) {
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 __device__ __forceinline__ unsigned long long entry_of(uint32_t key, int index) { return ((unsigned long long)key << 32) | (uint32_t)~index; }
 
+// s and u of a share, relative to its largest logit m: of t = (x - m) log2(e), s = sum 2^t, u = sum 2^t t.  The scaled base m log2(e)
+// is rounded once, b, and t = x log2(e) - b in one step: what that rounding moves it moves in every term and in the answers' own t alike.
+// Beyond kHuge, where that rounding is no small number any more, t is (x - m) log2(e).
 struct Sums {
     float m, s, u;
 };
+constexpr float kHuge = 1e6f;
+__device__ __forceinline__ bool small(float m) { return fabsf(m) <= kHuge; }
+// The logarithm of a probability from the sums of a row.
+__device__ __forceinline__ float log_of(float x, float m, float log2_s) {
+    constexpr float kLn2 = 0.6931471805599453f;
+    return small(m) && fabsf(x) <= 1e37f ? (fmaf(x, kLog2E, -__fmul_rn(m, kLog2E)) - log2_s) * kLn2 : (x - m) - log2_s * kLn2;
+}
+__device__ __forceinline__ float shift(float from, float to) {   // t of the old base over the new one
+    if (from == to) return 0.f;
+    const float old = __fmul_rn(from, kLog2E);
+    const float d = small(to) ? (small(from) ? __fsub_rn(old, __fmul_rn(to, kLog2E)) : fmaf(from, kLog2E, -__fmul_rn(to, kLog2E)))
+                              : (small(from) ? fmaf(-to, kLog2E, old) : (from - to) * kLog2E);
+    return fmaxf(d, kFar);
+}
 // The same sums over a larger maximum.
 __device__ __forceinline__ Sums lower(const Sums& a, float m) {
     if (a.m == m) return a;
-    const float d = fmaxf(a.m - m, kFar), e = exp_of(d);
+    const float d = shift(a.m, m), e = exp2_of(d);
     return {m, a.s * e, e * (a.u + d * a.s)};
 }
 __device__ __forceinline__ Sums join(const Sums& a, const Sums& b) {
@@ -107,37 +123,120 @@ __device__ __forceinline__ float largest(const Vec<__nv_bfloat16>& q) {
     return fmaxf(__low2float(m), __high2float(m));
 }
 
-// Sums over a base that stays, in pairs.
-struct Pairs {
-    f32x2 s, u;
-    __device__ Pairs() : s(0), u(0) {}
-    template <class T>
-    __device__ __forceinline__ void add(const Vec<T>& q, f32x2 minus_base) {
+// Logits of at most kLeast may be taken for it where the largest is above kFast: their exponentials are 0 all the same, and t stays finite.
+template <class T>
+struct Least;
+template <>
+struct Least<float> {
+    static constexpr float kLeast = -1e38f, kFast = -kHuge;
+    static __device__ __forceinline__ void clamp(Vec<float>& q) {
 #pragma unroll
-        for (int j = 0; j < Vec<T>::N; j += 2) {
-            float d0, d1, t0, t1;
-            unpack2(add2(pack2(to_float(q.v[j]), to_float(q.v[j + 1])), minus_base), d0, d1);
-            const f32x2 d = pack2(max_nan(d0, kFar), max_nan(d1, kFar));
-            unpack2(mul2(d, dup2(kLog2E)), t0, t1);
-            const f32x2 e = pack2(exp2_of(t0), exp2_of(t1));
-            s = add2(s, e);
-            fma2(u, e, d);
+        for (int j = 0; j < 4; ++j) q.v[j] = max_nan(q.v[j], kLeast);
+    }
+};
+template <>
+struct Least<__half> {
+    static constexpr float kLeast = -65504.f, kFast = -60000.f;
+    static __device__ __forceinline__ void clamp(Vec<__half>& q) {
+        __half2* w = reinterpret_cast<__half2*>(q.v);
+        const __half2 least = __float2half2_rn(kLeast);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = __hmax2_nan(w[j], least);
+    }
+};
+template <>
+struct Least<__nv_bfloat16> {
+    static constexpr float kLeast = -1e38f, kFast = -kHuge;
+    static __device__ __forceinline__ void clamp(Vec<__nv_bfloat16>& q) {
+        __nv_bfloat162* w = reinterpret_cast<__nv_bfloat162*>(q.v);
+        const __nv_bfloat162 least = __float2bfloat162_rn(kLeast);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = __hmax2_nan(w[j], least);
+    }
+};
+
+// Element e of a vector.
+template <class T>
+__device__ __forceinline__ float element(const Vec<T>& q, int e) {
+    const uint4 w = *reinterpret_cast<const uint4*>(q.v);
+    const int i = sizeof(T) == 4 ? e : e >> 1;
+    const uint32_t x = i & 2 ? (i & 1 ? w.w : w.z) : (i & 1 ? w.y : w.x);
+    if (sizeof(T) == 4) return __uint_as_float(x);
+    const unsigned short h = (unsigned short)(e & 1 ? x >> 16 : x);
+    T v;
+    *reinterpret_cast<unsigned short*>(&v) = h;
+    return to_float(v);
+}
+// A thread's sums, in pairs.
+struct Pairs {
+    float m;
+    f32x2 s, u;
+    __device__ Pairs() : m(-INFINITY), s(0), u(0) {}
+    __device__ __forceinline__ void term(f32x2 t) {
+        float t0, t1;
+        unpack2(t, t0, t1);
+        const f32x2 e = pack2(exp2_of(t0), exp2_of(t1));
+        s = add2(s, e);
+        fma2(u, e, t);
+    }
+    // The base for these, whose largest is returned, and what they add.
+    template <class T, int V>
+    __device__ __forceinline__ float raise(const Vec<T> (&q)[V]) {
+        float most = largest(q[0]);
+#pragma unroll
+        for (int i = 1; i < V; ++i) most = fmaxf(most, largest(q[i]));
+        if (most > m) {
+            const float d = shift(m, most), e = exp2_of(d);
+            fma2(u, dup2(d), s);
+            u = mul2(u, dup2(e));
+            s = mul2(s, dup2(e));
+            m = most;
+        }
+        return most;
+    }
+    // What the first `there` of them add.
+    template <class T, int V>
+    __device__ __forceinline__ void terms(Vec<T> (&q)[V], int there) {
+        if (m > Least<T>::kFast && m <= kHuge) {
+            const f32x2 scale = dup2(kLog2E), base = dup2(-__fmul_rn(m, kLog2E));
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                if (i >= there) break;
+                Least<T>::clamp(q[i]);
+#pragma unroll
+                for (int j = 0; j < Vec<T>::N; j += 2) {
+                    f32x2 t = base;
+                    fma2(t, pack2(to_float(q[i].v[j]), to_float(q[i].v[j + 1])), scale);
+                    term(t);
+                }
+            }
+        } else {   // rare, and little code: see take()
+            const bool huge = !small(m);
+            const float from = huge && m > -INFINITY ? m : 0.f, base = huge ? 0.f : -__fmul_rn(m, kLog2E);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+#pragma unroll 1
+                for (int j = 0; i < there && j < Vec<T>::N; j += 2)
+                    term(pack2(max_nan(fmaf(element(q[i], j) - from, kLog2E, base), kFar), max_nan(fmaf(element(q[i], j + 1) - from, kLog2E, base), kFar)));
         }
     }
-    __device__ __forceinline__ void lower_by(float d) {   // to a base larger by -d
-        const float e = exp_of(d);
-        fma2(u, dup2(d), s);
-        u = mul2(u, dup2(e));
-        s = mul2(s, dup2(e));
+    template <class T, int V>
+    __device__ __forceinline__ void add(Vec<T> (&q)[V]) {
+        raise(q);
+        terms(q, V);
     }
-    __device__ __forceinline__ Sums over(float m) const {
+    template <class T>
+    __device__ __forceinline__ void add(Vec<T> q) {
+        Vec<T> one[1] = {q};
+        add(one);
+    }
+    __device__ __forceinline__ Sums all() const {
         float a, b, c, d;
         unpack2(s, a, b);
         unpack2(u, c, d);
         return {m, a + b, c + d};
     }
 };
-__device__ __forceinline__ f32x2 minus_base(float m) { return dup2(m == -INFINITY ? 0.f : -m); }
 
 // A row as 16-byte vectors on 16-byte boundaries; the first and the last may lie partly outside it.
 template <class T>
@@ -176,7 +275,7 @@ template <int NT>
 struct Team {
     static constexpr int WARPS = NT / 32;
     static constexpr int GROUPS = NT == 32 ? 32 : 64;
-    static constexpr int CAP = NT == 32 ? 256 : 2048;
+    static constexpr int CAP = NT == 32 ? 256 : 1024;
     alignas(16) unsigned long long list[CAP];   // two at a time
     unsigned long long best[kMaxTop];
     Sums sums[WARPS], total;
@@ -211,24 +310,22 @@ __device__ __forceinline__ uint32_t bound_of(const Team<NT>& t, int top) {
         if (rank[h] < top) bound = min(bound, k[h]);
     return __reduce_min_sync(~0u, bound);
 }
-// The classes of a vector that reach the bound, into the list as far as it goes.
+// The classes of a vector that reach the bound, into the list as far as it goes.  (Little code, called from one place of a kernel: a row's
+// end runs it once a warp, and what is not in the instruction cache then is waited for.  Unrolled over the elements and at
+// several places it made the 20 most probable classes of 2048 x 131072 cost 61 us.)
 template <class T, int NT>
 __device__ __forceinline__ void take(Team<NT>& t, const Row<T>& row, const Vec<T>& q, int v, float bound) {
     uint32_t hits = 0;
 #pragma unroll
-    for (int e = 0; e < Vec<T>::N; ++e) hits |= (uint32_t)(to_float(q.v[e]) >= bound || bound == -INFINITY) << e;   // NaN counts as -inf
-    if (!hits) return;
-    if (v < row.full0 || v >= row.full1)
-#pragma unroll
-        for (int e = 0; e < Vec<T>::N; ++e)
-            if (!row.inside(v, e)) hits &= ~(1u << e);
-    int at = atomicAdd(&t.count, __popc(hits));
-#pragma unroll
-    for (int e = 0; e < Vec<T>::N; ++e)
-        if (hits >> e & 1) {
-            if (at < Team<NT>::CAP) t.list[at] = entry_of(key_of(to_float(q.v[e])), row.index(v, e));
-            ++at;
-        }
+    for (int e = 0; e < Vec<T>::N; ++e) hits |= (uint32_t)(to_float(q.v[e]) >= bound) << e;
+    if (bound == -INFINITY) hits = (1u << Vec<T>::N) - 1;   // NaN counts as -inf
+#pragma unroll 1
+    for (; hits; hits &= hits - 1) {
+        const int e = __ffs(hits) - 1;
+        if (!row.inside(v, e)) continue;
+        const int at = atomicAdd(&t.count, 1);
+        if (at < Team<NT>::CAP) t.list[at] = entry_of(key_of(element(q, e)), row.index(v, e));
+    }
 }
 
 // More classes reach the bound than the list holds: the first `top` of the vectors [v0, v1) of a row, without order, into t.list;
@@ -364,98 +461,16 @@ __device__ __forceinline__ V load_remote(const V* p, int rank) {
     return r;
 }
 
-// NT = 32: eight rows a CTA, a warp each; else a row, or with parts > 1 one of the parts of a row that a cluster shares.
-template <class T, int NT, bool RES>
-__global__ void __launch_bounds__(256, 4)
-logprobs_kernel(const Params p) {
-    constexpr int TEAMS = NT == 32 ? 8 : 1, WARPS = Team<NT>::WARPS, GL = NT / Team<NT>::GROUPS, U = 4;
-    __shared__ Team<NT> teams[TEAMS];
-    grid_dependency_wait();
-    grid_dependency_release();
-    Team<NT>& t = teams[threadIdx.x / NT];
+// What is left of a row, or of the part [v0, v1) of it that a CTA has, when every thread has its sums `a` (has: of at least one vector):
+// joins them, finds the most probable classes and, in the first part, writes the answers.  scan(reaches, least), called by whole warps,
+// takes what is least or more out of the shares of the threads that reach the bound.
+template <class T, int NT, class Scan>
+__device__ __forceinline__ void finish(Team<NT>& t, const Params& p, const Row<T>& row, int64_t r, int part, int v0, int v1, bool has, Sums a,
+                                       Scan scan) {
+    constexpr int WARPS = Team<NT>::WARPS, GL = NT / Team<NT>::GROUPS;
     const int id = threadIdx.x % NT, lane = id & 31, warp = id >> 5;
-    const int64_t r = NT == 32 ? (int64_t)blockIdx.x * TEAMS + threadIdx.x / NT : blockIdx.x / p.parts;
-    const int part = NT == 32 ? 0 : blockIdx.x % p.parts;
-    if (r >= p.rows) return;   // whole warps, and never part of a cluster
-    const Row<T> row(static_cast<const T*>(p.x) + r * p.ld, p.classes);
-    const int v0 = (int)((int64_t)row.vectors * part / p.parts), v1 = (int)((int64_t)row.vectors * (part + 1) / p.parts);
-    const int mine0 = v0 + id;
-
-    // the thread's share
-    Vec<T> held[RES ? kHeld : 1];
-    Sums a = {-INFINITY, 0.f, 0.f};
-    Pairs sums;
-    if (RES) {
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            const int v = mine0 + i * NT;
-            if (v < v1 && v >= row.full0 && v < row.full1) held[i] = row.load_full(v);
-            else held[i].fill(-INFINITY);
-        }
-        // the first and the last vector of the row may be partly outside it
-        for (int e = 0; e < 2; ++e) {
-            const int v = e ? row.vectors - 1 : 0;
-            if ((e ? row.full1 != row.vectors : row.full0) && v >= v0 && v < v1 && (v - v0) % NT == id) {
-                const Vec<T> q = row.load(v);
-#pragma unroll
-                for (int i = 0; i < kHeld; ++i)
-                    if (mine0 + i * NT == v) held[i] = q;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i) a.m = fmaxf(a.m, largest(held[i]));
-        const f32x2 base = minus_base(a.m);
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (mine0 + i * NT < v1) sums.add(held[i], base);
-    } else {
-        auto raise = [&](float m) {
-            if (m > a.m) {
-                sums.lower_by(fmaxf(a.m - m, kFar));
-                a.m = m;
-            }
-        };
-        auto one = [&](int v) {
-            const Vec<T> q = row.load(v);
-            raise(largest(q));
-            sums.add(q, minus_base(a.m));
-        };
-        int v = mine0;
-        if (v < v1) one(v);
-        v += NT;
-        const int end = min(v1, row.full1);
-        // U vectors are on their way while the U before them are added up
-        if (v + (U - 1) * NT < end) {
-            Vec<T> q[U];
-#pragma unroll
-            for (int i = 0; i < U; ++i) q[i] = row.load_full(v + i * NT);
-            v += U * NT;
-#pragma unroll 1
-            for (;;) {
-                const bool more = v + (U - 1) * NT < end;
-                Vec<T> next[U];
-                if (more)
-#pragma unroll
-                    for (int i = 0; i < U; ++i) next[i] = row.load_full(v + i * NT);
-                float m = largest(q[0]);
-#pragma unroll
-                for (int i = 1; i < U; ++i) m = fmaxf(m, largest(q[i]));
-                raise(m);
-                const f32x2 base = minus_base(a.m);
-#pragma unroll
-                for (int i = 0; i < U; ++i) sums.add(q[i], base);
-                if (!more) break;
-#pragma unroll
-                for (int i = 0; i < U; ++i) q[i] = next[i];
-                v += U * NT;
-            }
-        }
-        for (; v < v1; v += NT) one(v);
-    }
-    a = sums.over(a.m);
-
     // the groups' maxima; from them the row's, to which everybody brings down its sums, and the bound
-    const uint32_t mine = mine0 < v1 ? key_of(a.m) : 0u;
+    const uint32_t mine = has ? key_of(a.m) : 0u;
     uint32_t g = mine;
 #pragma unroll
     for (int o = 1; o < GL; o <<= 1) g = max(g, __shfl_xor_sync(~0u, g, o));
@@ -465,7 +480,7 @@ logprobs_kernel(const Params p) {
     uint32_t most = t.keys[lane];
     if (NT > 32) most = max(most, t.keys[lane + 32]);
     most = __reduce_max_sync(~0u, most);
-    a = lower(a, value_of(most));
+    a = lower(a, most ? value_of(most) : -INFINITY);
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         a.s += __shfl_xor_sync(~0u, a.s, o);
@@ -481,22 +496,7 @@ logprobs_kernel(const Params p) {
     }
     if (p.top) {
         const uint32_t bound = p.top == 1 ? most : NT == 32 ? bound_of<NT>(t, p.top) : t.bound;
-        // The lanes of a warp read the shares of those among them that reach the bound again, from the L1 or the L2: of four at
-        // a time where a share is no more than kHeld vectors.
-        constexpr int L = RES ? kHeld : 32;   // lanes that look at a share
-        const float least = bound ? value_of(bound) : -INFINITY;
-        const int share = (v1 - v0 + NT - 1) / NT;
-        for (uint32_t who = __ballot_sync(~0u, mine >= bound && mine); who;) {
-            int from = -1;
-#pragma unroll
-            for (int q = 0; q < 32 / L; ++q) {
-                if (lane / L == q && who) from = __ffs(who) - 1;
-                who &= who - 1;
-            }
-            const int first = __shfl_sync(~0u, mine0, from & 31);
-            if (from >= 0)
-                for (int j = lane % L, v = first + j * NT; j < share && v < v1; j += L, v += L * NT) take<T, NT>(t, row, row.load(v), v, least);
-        }
+        scan(mine >= bound && mine, bound ? value_of(bound) : -INFINITY);
         team_sync<NT>();
         int n = t.count;
         bool done = false;
@@ -516,6 +516,7 @@ logprobs_kernel(const Params p) {
         }
         if (p.parts > 1) {
             if (id == 0) t.total = a;
+            __syncwarp();
             cluster_sync();
             if (part == 0 && warp == 0) {
                 for (int c = 1; c < p.parts; ++c) {
@@ -529,24 +530,165 @@ logprobs_kernel(const Params p) {
                 __syncthreads();
                 order<NT, NT>(t, n, p.top, id);
             }
+            __syncwarp();
             cluster_sync();
         }
         if (part || warp) return;
     }
-    const float log_s = logf(a.s);
-    if (lane == 0 && p.entropy) p.entropy[r] = log_s - a.u / a.s;
+    const float log2_s = log2f(a.s);
+    if (lane == 0 && p.entropy) p.entropy[r] = (log2_s - a.u / a.s) * 0.6931471805599453f;
     for (int i = lane; i < p.ntargets; i += 32) {
         const int32_t c = p.targets[r * p.ntargets + i];
         float f = 0.f;
         if (c >= p.classes) f = NAN;
-        else if (c >= 0) f = (to_float(row.x[c]) - a.m) - log_s;
+        else if (c >= 0) f = log_of(to_float(row.x[c]), a.m, log2_s);
         p.logprob[r * p.ntargets + i] = f;
     }
     for (int i = lane; i < p.top; i += 32) {
         const unsigned long long c = t.best[i];
         p.top_index[r * p.top + i] = (int32_t)~(uint32_t)c;
-        p.top_logprob[r * p.top + i] = (value_of((uint32_t)(c >> 32)) - a.m) - log_s;
+        p.top_logprob[r * p.top + i] = log_of(value_of((uint32_t)(c >> 32)), a.m, log2_s);
     }
+}
+
+// Rows that the threads of a team hold (kHeld vectors a thread at most).  NT = 32: eight rows a CTA, a warp each; else a row, or
+// with parts > 1 one of the parts of a row that a cluster shares.
+template <class T, int NT>
+__global__ void __launch_bounds__(NT == 512 ? 512 : 256, NT == 512 ? 2 : 4)
+logprobs_held_kernel(const Params p) {
+    constexpr int TEAMS = NT == 32 ? 8 : 1;
+    __shared__ Team<NT> teams[TEAMS];
+    grid_dependency_wait();
+    grid_dependency_release();
+    Team<NT>& t = teams[threadIdx.x / NT];
+    const int id = threadIdx.x % NT;
+    const int64_t r = NT == 32 ? (int64_t)blockIdx.x * TEAMS + threadIdx.x / NT : blockIdx.x / p.parts;
+    const int part = NT == 32 ? 0 : blockIdx.x % p.parts;
+    if (r >= p.rows) return;   // whole warps, and never part of a cluster
+    const Row<T> row(static_cast<const T*>(p.x) + r * p.ld, p.classes);
+    const int v0 = (int)((int64_t)row.vectors * part / p.parts), v1 = (int)((int64_t)row.vectors * (part + 1) / p.parts);
+    const int mine0 = v0 + id;
+    Vec<T> held[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        const int v = mine0 + i * NT;
+        if (v < v1 && v >= row.full0 && v < row.full1) held[i] = row.load_full(v);
+        else held[i].fill(-INFINITY);
+    }
+    // the first and the last vector of the row may be partly outside it
+    for (int e = 0; e < 2; ++e) {
+        const int v = e ? row.vectors - 1 : 0;
+        if ((e ? row.full1 != row.vectors : row.full0) && v >= v0 && v < v1 && (v - v0) % NT == id) {
+            const Vec<T> q = row.load(v);
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if (mine0 + i * NT == v) held[i] = q;
+        }
+    }
+    Pairs sums;
+    sums.raise(held);   // places without a vector are -inf
+    sums.terms(held, mine0 < v1 ? (v1 - mine0 + NT - 1) / NT : 0);
+    finish<T, NT>(t, p, row, r, part, v0, v1, mine0 < v1, sums.all(), [&](bool reaches, float least) {
+        // eight lanes a share read it again, from the L1 or the L2
+        for (uint32_t who = __ballot_sync(~0u, reaches); who;) {
+            int from = -1;
+#pragma unroll
+            for (int q = 0; q < 32 / kHeld; ++q) {
+                if ((threadIdx.x & 31) / kHeld == q && who) from = __ffs(who) - 1;
+                who &= who - 1;
+            }
+            const int first = __shfl_sync(~0u, mine0, from & 31), v = first + (int)(threadIdx.x % kHeld) * NT;
+            if (from >= 0 && v < v1) take<T, NT>(t, row, row.load(v), v, least);
+        }
+    });
+}
+
+// Longer rows, or parts of them.  Every thread has a ring of its own in shared memory, which asynchronous copies fill: kAhead vectors
+// a group, two groups on their way while one is added up, 128 KB an SM (through registers it was half of that, and 2048 x 131072 bf16
+// took 114 us; bulk copies into a ring of the whole CTA, with barriers, 114).  The largest of a group, or of several, is kept (rounded
+// up to bf16), so that of the shares that reach the bound only the groups that do are read again.
+constexpr int kAhead = 4, kBuckets = 16;
+constexpr int kStreamSmem = 2 * kAhead * 256 * 16;
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+template <class T>
+__global__ void __launch_bounds__(256, 4)
+logprobs_stream_kernel(const Params p) {
+    constexpr int NT = 256, GROUP = kAhead * NT;
+    __shared__ Team<NT> t;
+    __shared__ __nv_bfloat16 tops[kBuckets][NT];
+    extern __shared__ uint4 ring[];   // [2][kAhead][NT]
+    grid_dependency_wait();
+    grid_dependency_release();
+    const int id = threadIdx.x, lane = id & 31;
+    const int64_t r = blockIdx.x / p.parts;
+    const int part = blockIdx.x % p.parts;
+    const Row<T> row(static_cast<const T*>(p.x) + r * p.ld, p.classes);
+    const int v0 = (int)((int64_t)row.vectors * part / p.parts), v1 = (int)((int64_t)row.vectors * (part + 1) / p.parts);
+    const int mine0 = v0 + id, end = min(v1, row.full1);
+    // A thread's first vector, which may be partly outside the row, then whole groups of vectors, then what is left.
+    auto groups_of = [&](int first) { return max(0, (end - first - 1) / GROUP); };
+    const int groups = groups_of(mine0);
+    int wide = 0;   // 2^wide groups share a bucket; the last bucket is for the vectors that are in no group
+    while ((groups_of(v0) >> wide) >= kBuckets - 1) ++wide;
+
+    const uint4* const from = reinterpret_cast<const uint4*>(row.x - row.lead) + mine0 + NT;
+    const uint32_t slots = smem_u32(ring + id);
+    auto ask = [&](int g) {
+        if (g < groups)
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) copy16(slots + (uint32_t)(((g & 1) * kAhead + i) * NT * 16), from + (int64_t)g * GROUP + i * NT);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    ask(0);
+    ask(1);
+    Pairs sums;
+    float others = -INFINITY, top = -INFINITY;
+    auto alone = [&](int v) {
+        const Vec<T> q = row.load(v);
+        others = fmaxf(others, largest(q));
+        sums.add(q);
+    };
+    if (mine0 < v1) alone(mine0);
+#pragma unroll 1
+    for (int g = 0; g < groups; ++g) {
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        Vec<T> q[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) *reinterpret_cast<uint4*>(q[i].v) = ring[((g & 1) * kAhead + i) * NT + id];
+        const float most = sums.raise(q);   // what was read from the ring is in registers now
+        ask(g + 2);
+        top = fmaxf(top, most);
+        if (((g + 1) & ((1 << wide) - 1)) == 0 || g + 1 == groups) {
+            tops[g >> wide][id] = __float2bfloat16_ru(top);
+            top = -INFINITY;
+        }
+        sums.terms(q, kAhead);
+    }
+    for (int v = mine0 + NT + groups * GROUP; v < v1; v += NT) alone(v);
+    tops[kBuckets - 1][id] = __float2bfloat16_ru(others);
+    asm volatile("cp.async.wait_all;" ::: "memory");
+
+    finish<T, NT>(t, p, row, r, part, v0, v1, mine0 < v1, sums.all(), [&](bool reaches, float least) {
+        // share by share: a lane a bucket, then a lane a vector of those that reach it
+        for (uint32_t who = __ballot_sync(~0u, reaches); who; who &= who - 1) {
+            const int other = (id & ~31) + __ffs(who) - 1, first = v0 + other, n = groups_of(first);
+            const bool hit = lane < kBuckets && (lane == kBuckets - 1 || (lane << wide) < n) && __bfloat162float(tops[lane % kBuckets][other]) >= least;
+            for (uint32_t which = __ballot_sync(~0u, hit); which; which &= which - 1) {
+                const int b = __ffs(which) - 1, tail = first + NT + n * GROUP;
+                // the last bucket: the first vector and those behind the groups
+                const int from = b == kBuckets - 1 ? tail - NT : first + NT + (b << wide) * GROUP;
+                const int last = b == kBuckets - 1 ? v1 : first + NT + min(n, (b + 1) << wide) * GROUP;
+#pragma unroll 1
+                for (int i = lane; from + i * NT < last; i += 32) {
+                    const int v = b == kBuckets - 1 && i == 0 ? first : from + i * NT;
+                    take<T, NT>(t, row, row.load(v), v, least);
+                }
+            }
+        }
+    });
 }
 
 template <class T>
@@ -558,15 +700,28 @@ sbnn_status launch_as(const Params& given, cudaStream_t st) {
     const int sms = device_sms();
     p.parts = 1;
     ChainedLaunchScope chained;
-    if (vectors <= 32 * kHeld && p.rows >= 8 * sms) {
-        SBNN_CUDA_TRY(launch_kernel(logprobs_kernel<T, 32, true>, dim3((unsigned)((p.rows + 7ll) / 8)), dim3(256), 0, st, p));
+    // A warp a row: 64 x 1000 fp32 top 5 4.0 us (a CTA a row 4.3), 1000 x 1000 bf16 4.7 (10.2); but for many alternatives of few rows a CTA
+    // has the tighter bound: 64 x 1000 top 20 6.7 (4.7).
+    if (vectors <= 32 * kHeld && (p.top <= 8 || p.rows > 2 * sms)) {
+        SBNN_CUDA_TRY(launch_kernel(logprobs_held_kernel<T, 32>, dim3((unsigned)((p.rows + 7ll) / 8)), dim3(256), 0, st, p));
         return SBNN_OK;
     }
+    // Few rows are shared by clusters: 100 x 262144 fp32 by 1, 2 and 4 CTAs 35, 28 and 28 us, 16 rows 28, 20 and 15, 300 x 100000 34, 43
+    // and 52.
     while (p.parts < 8 && (int64_t)p.rows * p.parts * 2 <= 2 * sms && vectors / (p.parts * 2) >= 256) p.parts *= 2;
     if ((int64_t)p.rows * p.parts > 0x7fffffff) return fail(SBNN_ERR_SHAPE, "too many rows");
-    // a part has at most one vector more than its share
-    auto* const kernel = (vectors + p.parts - 1) / p.parts <= 256 * kHeld ? logprobs_kernel<T, 256, true> : logprobs_kernel<T, 256, false>;
-    SBNN_CUDA_TRY(launch_kernel_cluster(kernel, dim3((unsigned)(p.rows * p.parts)), dim3(256), 0, st, (unsigned)p.parts, p));
+    const dim3 grid((unsigned)(p.rows * p.parts));
+    const int64_t share = (vectors + p.parts - 1) / p.parts;
+    // 512 threads hold a share where all run at once: 200 x 32000 bf16 7.6 us (streamed 10.9), 3166 x 20000 47 (38)
+    if (share <= 256 * kHeld) {
+        SBNN_CUDA_TRY(launch_kernel_cluster(logprobs_held_kernel<T, 256>, grid, dim3(256), 0, st, (unsigned)p.parts, p));
+    } else if (share <= 512 * kHeld && (int64_t)p.rows * p.parts <= 2 * sms) {
+        SBNN_CUDA_TRY(launch_kernel_cluster(logprobs_held_kernel<T, 512>, grid, dim3(512), 0, st, (unsigned)p.parts, p));
+    } else {
+        const sbnn_status r = set_max_dyn_smem(reinterpret_cast<const void*>(&logprobs_stream_kernel<T>), kStreamSmem);
+        if (r != SBNN_OK) return r;
+        SBNN_CUDA_TRY(launch_kernel_cluster(logprobs_stream_kernel<T>, grid, dim3(256), (size_t)kStreamSmem, st, (unsigned)p.parts, p));
+    }
     return SBNN_OK;
 }
 
