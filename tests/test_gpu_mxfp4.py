@@ -59,7 +59,8 @@ def check_quantize(x, ld=None):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("m,k", [(1, 1), (1, 31), (1, 32), (2, 33), (1, 1024), (5, 129), (33, 96), (127, 128), (128, 160), (129, 517), (300, 256), (257, 1000)])
+@pytest.mark.parametrize("m,k", [(1, 1), (1, 31), (1, 32), (2, 33), (1, 1024), (5, 129), (33, 96), (127, 128), (128, 160), (129, 517), (300, 256), (257, 1000),
+                                 (40000, 40), (38000, 64), (39000, 100), (37890, 128), (9000, 1001), (4800, 2048)])
 def test_quantize_is_exact(m, k, dtype):
     check_quantize(activations(m, k, dtype, 7 * m + k))
 
@@ -95,7 +96,8 @@ def test_quantize_special_values(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("m,k,ld", [(1, 1, 1), (1, 1000, 1000), (129, 517, 517), (129, 517, 530), (40, 256, 264), (256, 96, 96)])
+@pytest.mark.parametrize("m,k,ld", [(1, 1, 1), (1, 1000, 1000), (129, 517, 517), (129, 517, 530), (40, 256, 264), (256, 96, 96), (37900, 33, 33), (38000, 64, 64), (37888, 120, 121),
+                                    (37889, 128, 128), (9000, 1001, 1001), (4800, 2048, 2056)])
 def test_dequantize_is_the_value_rounded_once(m, k, ld, dtype):
     rng = np.random.default_rng(m + k)
     codes = rng.integers(0, 256, (m, 16 * O.blocks_of(k))).astype(np.uint8)
