@@ -12,17 +12,18 @@ namespace sbnn {
 namespace {
 
 // LPR lanes take a row, eight channels a lane: all 32 of a warp, or 16 or 8 where rows are no longer than 128 or 64 channels (60000 x 64 bf16
-// with 32: 10 us either way).  A warp has up to kAhead loads a lane on their way.  A CTA of eight warps has 8 RPW rows: 128, so that
+// with 32: 10 us either way).  Of codes a warp has up to eight loads a lane on their way, of values four, which leaves
+// room for more warps (16384 x 8192 fp32 to 4 bits: 89 us, with eight 104).  A CTA of eight warps has 8 RPW rows: 128, so that
 // its scales are whole tiles, or 32 where that leaves SMs without one.  Scales are gathered in shared memory.  Rows that
 // do not start on 16 bytes, or do not end with a whole vector, are read and written one element a lane and pass through
 // shared memory (20000 x 1001 bf16 21.7 and 13.5 us there and back; through eight loads a lane 86 together).  Four warps side by side
 // in a row instead of below each other took 66 and 66 us for 16384 x 8192 bf16, like this 64 and 57.
-constexpr int kThreads = 256, kAhead = 8;
+constexpr int kThreads = 256, kAhead = 8, kRead = 4;
 
 template <class T, bool VEC, int LPR, int RPW>
 __global__ void __launch_bounds__(kThreads)
 quantize_kernel(const T* __restrict__ x, int64_t ldx, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, int M, int K, int ktiles) {
-    constexpr int ROWS = 8 * RPW, AT = 32 / LPR, BATCH = RPW / AT < kAhead ? RPW / AT : kAhead;   // AT: rows of a warp side by side
+    constexpr int ROWS = 8 * RPW, AT = 32 / LPR, BATCH = RPW / AT < kRead ? RPW / AT : kRead;   // AT: rows of a warp side by side
     __shared__ uint32_t tile[2][ROWS];   // [k-tile][row of the CTA]: four scale bytes each
     __shared__ Eight<T> turn[VEC ? 1 : kThreads];
     grid_dependency_wait();
