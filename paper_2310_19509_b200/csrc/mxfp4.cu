@@ -12,18 +12,16 @@ namespace sbnn {
 namespace {
 
 // LPR lanes take a row, eight channels a lane: all 32 of a warp, or 16 or 8 where rows are no longer than 128 or 64 channels (60000 x 64 bf16
-// with 32: 10 us either way).  Of codes a warp has up to eight loads a lane on their way, of values four, which leaves
-// room for more warps (16384 x 8192 fp32 to 4 bits: 89 us, with eight 104).  A CTA of eight warps has 8 RPW rows: 128, so that
-// its scales are whole tiles, or 32 where that leaves SMs without one.  Scales are gathered in shared memory.  Rows that
-// do not start on 16 bytes, or do not end with a whole vector, are read and written one element a lane and pass through
-// shared memory (20000 x 1001 bf16 21.7 and 13.5 us there and back; through eight loads a lane 86 together).  Four warps side by side
-// in a row instead of below each other took 66 and 66 us for 16384 x 8192 bf16, like this 64 and 57.
-constexpr int kThreads = 256, kAhead = 8, kRead = 4;
+// to 4 bits 3.4 us, with 32 lanes 10).  A warp has four rows, whose loads are all on their way before the first is used, a CTA 32.
+// (16 rows a warp, so that a CTA's scales are whole tiles: 16384 x 1024 bf16 14.8 us, like this 9.2; 16384 x 8192 fp32 89 and 87.)
+// Rows that do not start on 16 bytes, or do not end with a whole vector, are read and written one element a lane and pass
+// through shared memory (20000 x 1001 bf16 14.8 and 12.4 us there and back; through eight loads a lane 86 together).
+constexpr int kThreads = 256, kRows = 4;
 
-template <class T, bool VEC, int LPR, int RPW>
+template <class T, bool VEC, int LPR>
 __global__ void __launch_bounds__(kThreads)
 quantize_kernel(const T* __restrict__ x, int64_t ldx, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, int M, int K, int ktiles) {
-    constexpr int ROWS = 8 * RPW, AT = 32 / LPR, BATCH = RPW / AT < kRead ? RPW / AT : kRead;   // AT: rows of a warp side by side
+    constexpr int ROWS = 8 * kRows, AT = 32 / LPR, BATCH = kRows / AT;   // AT: rows of a warp side by side
     __shared__ uint32_t tile[2][ROWS];   // [k-tile][row of the CTA]: four scale bytes each
     __shared__ Eight<T> turn[VEC ? 1 : kThreads];
     grid_dependency_wait();
@@ -34,61 +32,57 @@ quantize_kernel(const T* __restrict__ x, int64_t ldx, uint8_t* __restrict__ code
     const int rows = (int)min((int64_t)ROWS, M - row0), k0 = kt * 128;
     const int64_t ldc = 16 * (int64_t)mx_blocks(K);
     const bool word = ((k0 + l * 8) & ~31) < K;   // the lane's word of codes exists
-#pragma unroll 1
-    for (int first = warp * RPW; first < min(rows, (warp + 1) * RPW); first += BATCH * AT) {
-        Eight<T> e[BATCH];   // VEC: channels k0 + 8 l ..; else channel k0 + l + LPR j
+    const int first = warp * kRows;
+    Eight<T> e[BATCH];   // VEC: channels k0 + 8 l ..; else channel k0 + l + LPR j
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int r = first + i * AT + at;
-            const T* p = x + (row0 + r) * ldx + k0;
-            if (VEC) {
-                if (r < rows && k0 + l * 8 < K) {
-                    load8<true>(e[i], p + l * 8, 8);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) e[i].v[j] = from_float<T>(0.f);
-                }
+    for (int i = 0; i < BATCH; ++i) {
+        const int r = first + i * AT + at;
+        const T* p = x + (row0 + r) * ldx + k0;
+        if (VEC) {
+            if (r < rows && k0 + l * 8 < K) {
+                load8<true>(e[i], p + l * 8, 8);
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) e[i].v[j] = r < rows && k0 + l + LPR * j < K ? __ldg(p + l + LPR * j) : from_float<T>(0.f);
+                for (int j = 0; j < 8; ++j) e[i].v[j] = from_float<T>(0.f);
             }
-        }
+        } else {
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int r = first + i * AT + at;
-            if (!VEC) {
-                Eight<T>* const row = turn + (threadIdx.x - l);
-                __syncwarp();
-#pragma unroll
-                for (int j = 0; j < 8; ++j) row[0].v[l + LPR * j] = e[i].v[j];
-                __syncwarp();
-                e[i] = row[l];
-            }
-            uint32_t m = largest_bits(e[i]);
-            m = max(m, __shfl_xor_sync(~0u, m, 1));
-            m = max(m, __shfl_xor_sync(~0u, m, 2));
-            const uint32_t byte = mx_scale_byte(m), c = encode8(e[i], byte);
-            // one lane of each quad has a block's byte: four lanes' make a word.  Blocks behind the last channel are all zeros: byte 0.
-            uint32_t w = byte << 8 * (l >> 2 & 3);
-            w |= __shfl_xor_sync(~0u, w, 4);
-            if (LPR > 8) w |= __shfl_xor_sync(~0u, w, 8);
-            if (r < rows && word) *reinterpret_cast<uint32_t*>(codes + (row0 + r) * ldc + (k0 >> 1) + l * 4) = c;
-            if ((l & 15) == 0 && r < rows) tile[l >> 4][r] = w;
+            for (int j = 0; j < 8; ++j) e[i].v[j] = r < rows && k0 + l + LPR * j < K ? __ldg(p + l + LPR * j) : from_float<T>(0.f);
         }
     }
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+        const int r = first + i * AT + at;
+        if (!VEC) {
+            Eight<T>* const row = turn + (threadIdx.x - l);
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) row[0].v[l + LPR * j] = e[i].v[j];
+            __syncwarp();
+            e[i] = row[l];
+        }
+        uint32_t m = largest_bits(e[i]);
+        m = max(m, __shfl_xor_sync(~0u, m, 1));
+        m = max(m, __shfl_xor_sync(~0u, m, 2));
+        const uint32_t byte = mx_scale_byte(m), c = encode8(e[i], byte);
+        // one lane of each quad has a block's byte: four lanes' make a word.  Blocks behind the last channel are all zeros: byte 0.
+        uint32_t w = byte << 8 * (l >> 2 & 3);
+        w |= __shfl_xor_sync(~0u, w, 4);
+        if (LPR > 8) w |= __shfl_xor_sync(~0u, w, 8);
+        if (r < rows && word) *reinterpret_cast<uint32_t*>(codes + (row0 + r) * ldc + (k0 >> 1) + l * 4) = c;
+        if ((l & 15) == 0) tile[l >> 4][r] = w;
+    }
+    // (stored by the warps as they have them, a word of two lanes a row: 16384 x 8192 bf16 74 us, like this 63)
     __syncthreads();
-    // word t of a tile belongs to row t / 4 + 32 (t % 4) of it
-    for (int t = threadIdx.x; t < (LPR == 32 ? 2 : 1) * ROWS; t += kThreads) {
-        const int h = t / ROWS, w = t % ROWS, r = ROWS == 128 ? (w >> 2) + 32 * (w & 3) : w;
-        if (r < rows && kt + h < ktiles)
-            *reinterpret_cast<uint32_t*>(scales + mx_scale_offset(row0 + r, 4 * (kt + h), ktiles)) = tile[h][r];
-    }
+    const int h = threadIdx.x / ROWS, r = threadIdx.x % ROWS;
+    if (threadIdx.x < (LPR == 32 ? 2 : 1) * ROWS && r < rows && kt + h < ktiles)
+        *reinterpret_cast<uint32_t*>(scales + mx_scale_offset(row0 + r, 4 * (kt + h), ktiles)) = tile[h][r];
 }
 
-template <class T, bool VEC, int LPR, int RPW>
+template <class T, bool VEC, int LPR>
 __global__ void __launch_bounds__(kThreads)
 dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ y, int64_t ldy, int M, int K, int ktiles) {
-    constexpr int ROWS = 8 * RPW, AT = 32 / LPR, BATCH = RPW / AT < kAhead ? RPW / AT : kAhead;
+    constexpr int ROWS = 8 * kRows, AT = 32 / LPR, BATCH = kRows / AT;
     __shared__ Eight<T> turn[VEC ? 1 : kThreads];
     grid_dependency_wait();
     grid_dependency_release();
@@ -98,58 +92,57 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
     const int rows = (int)min((int64_t)ROWS, M - row0), k0 = kt * 128;
     const int64_t ldc = 16 * (int64_t)mx_blocks(K);
     const bool word = ((k0 + l * 8) & ~31) < K;
-#pragma unroll 1
-    for (int first = warp * RPW; first < min(rows, (warp + 1) * RPW); first += BATCH * AT) {
-        uint32_t c[BATCH], s[BATCH];   // a word of codes, the scales of the four blocks that it is one of
+    const int first = warp * kRows;
+    if (first >= rows) return;
+    uint32_t c[BATCH], s[BATCH];   // a word of codes, the scales of the four blocks that it is one of
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int r = first + i * AT + at;
-            c[i] = s[i] = 0;
-            if (r < rows && word) {
-                c[i] = __ldg(reinterpret_cast<const uint32_t*>(codes + (row0 + r) * ldc + (k0 >> 1) + l * 4));
-                s[i] = __ldg(reinterpret_cast<const uint32_t*>(scales + mx_scale_offset(row0 + r, 4 * (kt + (l >> 4)), ktiles)));
-            }
+    for (int i = 0; i < BATCH; ++i) {
+        const int r = first + i * AT + at;
+        c[i] = s[i] = 0;
+        if (r < rows && word) {
+            c[i] = __ldg(reinterpret_cast<const uint32_t*>(codes + (row0 + r) * ldc + (k0 >> 1) + l * 4));
+            s[i] = __ldg(reinterpret_cast<const uint32_t*>(scales + mx_scale_offset(row0 + r, 4 * (kt + (l >> 4)), ktiles)));
         }
+    }
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int r = first + i * AT + at;
-            T* p = y + (row0 + r) * ldy + k0;
-            constexpr bool LINES = VEC && sizeof(T) == 4 && LPR == 32;
-            float s0, s1;   // of the first and the last four of the lane's channels
-            if (LINES) {
-                // fp32: channels 4 l .. and 128 + 4 l .., so that both stores are whole lines (16384 x 8192: 99 us, 140 without)
-                const uint32_t a = __shfl_sync(~0u, c[i], l >> 1), b = __shfl_sync(~0u, c[i], 16 + (l >> 1));
-                const uint32_t sa = __shfl_sync(~0u, s[i], 0), sb = __shfl_sync(~0u, s[i], 16);
-                c[i] = l & 1 ? (a >> 16) | (b & 0xFFFF0000u) : (a & 0xFFFFu) | (b << 16);
-                s0 = mx_scale(sa >> 8 * (l >> 3) & 255u);
-                s1 = mx_scale(sb >> 8 * (l >> 3) & 255u);
-            } else {
-                s0 = s1 = mx_scale(s[i] >> 8 * (l >> 2 & 3) & 255u);
-            }
-            __half2 h[4];
-            mx_decode8(c[i], h);
-            Eight<T> e;
+    for (int i = 0; i < BATCH; ++i) {
+        const int r = first + i * AT + at;
+        T* p = y + (row0 + r) * ldy + k0;
+        constexpr bool LINES = VEC && sizeof(T) == 4 && LPR == 32;
+        float s0, s1;   // of the first and the last four of the lane's channels
+        if (LINES) {
+            // fp32: channels 4 l .. and 128 + 4 l .., so that both stores are whole lines (16384 x 8192: 99 us, 140 without)
+            const uint32_t a = __shfl_sync(~0u, c[i], l >> 1), b = __shfl_sync(~0u, c[i], 16 + (l >> 1));
+            const uint32_t sa = __shfl_sync(~0u, s[i], 0), sb = __shfl_sync(~0u, s[i], 16);
+            c[i] = l & 1 ? (a >> 16) | (b & 0xFFFF0000u) : (a & 0xFFFFu) | (b << 16);
+            s0 = mx_scale(sa >> 8 * (l >> 3) & 255u);
+            s1 = mx_scale(sb >> 8 * (l >> 3) & 255u);
+        } else {
+            s0 = s1 = mx_scale(s[i] >> 8 * (l >> 2 & 3) & 255u);
+        }
+        __half2 h[4];
+        mx_decode8(c[i], h);
+        Eight<T> e;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 f = __half22float2(h[j]);
-                e.v[2 * j] = from_float<T>(f.x * (j < 2 ? s0 : s1));
-                e.v[2 * j + 1] = from_float<T>(f.y * (j < 2 ? s0 : s1));
-            }
-            if (LINES) {
-                const float4* const f = reinterpret_cast<const float4*>(e.v);
-                if (r < rows && k0 + 4 * l < K) *reinterpret_cast<float4*>(p + 4 * l) = f[0];
-                if (r < rows && k0 + 128 + 4 * l < K) *reinterpret_cast<float4*>(p + 128 + 4 * l) = f[1];
-            } else if (VEC) {
-                if (r < rows && k0 + l * 8 < K) store8<true>(e, p + l * 8, 8);
-            } else {
-                Eight<T>* const row = turn + (threadIdx.x - l);
-                __syncwarp();
-                row[l] = e;
-                __syncwarp();
+        for (int j = 0; j < 4; ++j) {
+            const float2 f = __half22float2(h[j]);
+            e.v[2 * j] = from_float<T>(f.x * (j < 2 ? s0 : s1));
+            e.v[2 * j + 1] = from_float<T>(f.y * (j < 2 ? s0 : s1));
+        }
+        if (LINES) {
+            const float4* const f = reinterpret_cast<const float4*>(e.v);
+            if (r < rows && k0 + 4 * l < K) *reinterpret_cast<float4*>(p + 4 * l) = f[0];
+            if (r < rows && k0 + 128 + 4 * l < K) *reinterpret_cast<float4*>(p + 128 + 4 * l) = f[1];
+        } else if (VEC) {
+            if (r < rows && k0 + l * 8 < K) store8<true>(e, p + l * 8, 8);
+        } else {
+            Eight<T>* const row = turn + (threadIdx.x - l);
+            __syncwarp();
+            row[l] = e;
+            __syncwarp();
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (r < rows && k0 + l + LPR * j < K) p[l + LPR * j] = row[0].v[l + LPR * j];
-            }
+            for (int j = 0; j < 8; ++j)
+                if (r < rows && k0 + l + LPR * j < K) p[l + LPR * j] = row[0].v[l + LPR * j];
         }
     }
 }
@@ -165,46 +158,40 @@ sbnn_status check_matrix(const char* what, const void* p, int type, int64_t ld, 
     return SBNN_OK;
 }
 
-// Rows of a warp (16 or 4), lanes of a row (32, 16 or 8), and the CTAs.
-struct Shape {
-    int rpw, lpr;
-    unsigned blocks;
-};
-sbnn_status shape_of(int M, int K, Shape* s) {
-    const int64_t wide = (mx_ktiles(K) + 1) / 2;
-    s->lpr = K > 128 ? 32 : K > 64 ? 16 : 8;
-    s->rpw = ((int64_t)M + 127) / 128 * wide >= 2 * device_sms() ? 16 : 4;
-    const int64_t n = ((int64_t)M + 8 * s->rpw - 1) / (8 * s->rpw) * wide;
+// Lanes of a row, and the CTAs.
+sbnn_status grid_of(int M, int K, int* lpr, unsigned* blocks) {
+    *lpr = K > 128 ? 32 : K > 64 ? 16 : 8;
+    const int64_t n = ((int64_t)M + 8 * kRows - 1) / (8 * kRows) * ((mx_ktiles(K) + 1) / 2);
     if (n > 0x7fffffff) return fail(SBNN_ERR_SHAPE, "tensor too large");
-    s->blocks = (unsigned)n;
+    *blocks = (unsigned)n;
     return SBNN_OK;
 }
 
-template <class T, bool VEC, int RPW>
-auto quantize_for(int lpr) { return lpr == 32 ? quantize_kernel<T, VEC, 32, RPW> : lpr == 16 ? quantize_kernel<T, VEC, 16, RPW> : quantize_kernel<T, VEC, 8, RPW>; }
-template <class T, bool VEC, int RPW>
-auto dequantize_for(int lpr) { return lpr == 32 ? dequantize_kernel<T, VEC, 32, RPW> : lpr == 16 ? dequantize_kernel<T, VEC, 16, RPW> : dequantize_kernel<T, VEC, 8, RPW>; }
+template <class T, bool VEC>
+auto quantize_for(int lpr) { return lpr == 32 ? quantize_kernel<T, VEC, 32> : lpr == 16 ? quantize_kernel<T, VEC, 16> : quantize_kernel<T, VEC, 8>; }
+template <class T, bool VEC>
+auto dequantize_for(int lpr) { return lpr == 32 ? dequantize_kernel<T, VEC, 32> : lpr == 16 ? dequantize_kernel<T, VEC, 16> : dequantize_kernel<T, VEC, 8>; }
 
 template <class T>
 sbnn_status quantize_as(const void* x, int64_t ldx, uint8_t* codes, uint8_t* scales, int M, int K, cudaStream_t st) {
-    Shape s;
-    const sbnn_status r = shape_of(M, K, &s);
+    int lpr;
+    unsigned blocks;
+    const sbnn_status r = grid_of(M, K, &lpr, &blocks);
     if (r != SBNN_OK) return r;
-    auto* const kernel = whole_vectors(x, ldx, K, sizeof(T)) ? (s.rpw == 16 ? quantize_for<T, true, 16>(s.lpr) : quantize_for<T, true, 4>(s.lpr))
-                                                             : (s.rpw == 16 ? quantize_for<T, false, 16>(s.lpr) : quantize_for<T, false, 4>(s.lpr));
+    auto* const kernel = whole_vectors(x, ldx, K, sizeof(T)) ? quantize_for<T, true>(lpr) : quantize_for<T, false>(lpr);
     ChainedLaunchScope chained;
-    SBNN_CUDA_TRY(launch_kernel(kernel, dim3(s.blocks), dim3(kThreads), 0, st, static_cast<const T*>(x), ldx, codes, scales, M, K, mx_ktiles(K)));
+    SBNN_CUDA_TRY(launch_kernel(kernel, dim3(blocks), dim3(kThreads), 0, st, static_cast<const T*>(x), ldx, codes, scales, M, K, mx_ktiles(K)));
     return SBNN_OK;
 }
 template <class T>
 sbnn_status dequantize_as(const uint8_t* codes, const uint8_t* scales, void* y, int64_t ldy, int M, int K, cudaStream_t st) {
-    Shape s;
-    const sbnn_status r = shape_of(M, K, &s);
+    int lpr;
+    unsigned blocks;
+    const sbnn_status r = grid_of(M, K, &lpr, &blocks);
     if (r != SBNN_OK) return r;
-    auto* const kernel = whole_vectors(y, ldy, K, sizeof(T)) ? (s.rpw == 16 ? dequantize_for<T, true, 16>(s.lpr) : dequantize_for<T, true, 4>(s.lpr))
-                                                             : (s.rpw == 16 ? dequantize_for<T, false, 16>(s.lpr) : dequantize_for<T, false, 4>(s.lpr));
+    auto* const kernel = whole_vectors(y, ldy, K, sizeof(T)) ? dequantize_for<T, true>(lpr) : dequantize_for<T, false>(lpr);
     ChainedLaunchScope chained;
-    SBNN_CUDA_TRY(launch_kernel(kernel, dim3(s.blocks), dim3(kThreads), 0, st, codes, scales, static_cast<T*>(y), ldy, M, K, mx_ktiles(K)));
+    SBNN_CUDA_TRY(launch_kernel(kernel, dim3(blocks), dim3(kThreads), 0, st, codes, scales, static_cast<T*>(y), ldy, M, K, mx_ktiles(K)));
     return SBNN_OK;
 }
 
