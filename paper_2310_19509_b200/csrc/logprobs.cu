@@ -275,10 +275,11 @@ template <int NT>
 struct Team {
     static constexpr int WARPS = NT / 32;
     static constexpr int GROUPS = NT == 32 ? 32 : 64;
-    static constexpr int CAP = NT == 32 ? 256 : 1024;
-    alignas(16) unsigned long long list[CAP];   // two at a time
+    static constexpr int CAP = NT == 32 ? 256 : 768;   // candidates; behind them, in the first part's memory, the answers of a row's parts
+    alignas(16) unsigned long long list[NT == 32 ? CAP : CAP + 8 * kMaxTop];   // two at a time
     unsigned long long best[kMaxTop];
-    Sums sums[WARPS], total;
+    Sums sums[WARPS];
+    Sums part_sums[NT == 32 ? 1 : 8];
     alignas(16) uint32_t keys[GROUPS];   // read four at a time
     uint32_t bound;
     int scan[WARPS];
@@ -439,32 +440,24 @@ __device__ __forceinline__ void order(Team<NT>& t, int n, int top, int id) {
     else __syncthreads();
 }
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-template <class V>
-__device__ __forceinline__ V load_remote(const V* p, int rank) {
-    static_assert(sizeof(V) == 4 || sizeof(V) == 8, "one word");
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// Stores where the first CTA of the cluster has `p`.
+__device__ __forceinline__ void store_remote(const void* p, uint32_t v) {
     uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
-    V r;
-    if (sizeof(V) == 4) {
-        uint32_t w;
-        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(w) : "r"(a) : "memory");
-        *reinterpret_cast<uint32_t*>(&r) = w;
-    } else {
-        unsigned long long w;
-        asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(w) : "r"(a) : "memory");
-        *reinterpret_cast<unsigned long long*>(&r) = w;
-    }
-    return r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(0));
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+}
+__device__ __forceinline__ void store_remote(const void* p, unsigned long long v) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(0));
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
 }
 
 // What is left of a row, or of the part [v0, v1) of it that a CTA has, when every thread has its sums `a` (has: of at least one vector):
 // joins them, finds the most probable classes and, in the first part, writes the answers.  scan(reaches, least), called by whole warps,
 // takes what is least or more out of the shares of the threads that reach the bound.
-template <class T, int NT, class Scan>
+template <class T, int NT, bool SHARED, class Scan>
 __device__ __forceinline__ void finish(Team<NT>& t, const Params& p, const Row<T>& row, int64_t r, int part, int v0, int v1, bool has, Sums a,
                                        Scan scan) {
     constexpr int WARPS = Team<NT>::WARPS, GL = NT / Team<NT>::GROUPS;
@@ -514,26 +507,33 @@ __device__ __forceinline__ void finish(Team<NT>& t, const Params& p, const Row<T
             }
             a.s = __shfl_sync(~0u, a.s, 0), a.u = __shfl_sync(~0u, a.u, 0);
         }
-        if (p.parts > 1) {
-            if (id == 0) t.total = a;
-            __syncwarp();
-            cluster_sync();
-            if (part == 0 && warp == 0) {
-                for (int c = 1; c < p.parts; ++c) {
-                    const Sums b = {load_remote(&t.total.m, c), load_remote(&t.total.s, c), load_remote(&t.total.u, c)};
-                    a = join(a, b);
+        if (SHARED && p.parts > 1) {
+            // the parts' answers go to the first part's memory; only that waits for the others, which end here
+            cluster_wait();   // all CTAs of the cluster have begun
+            if (warp == 0) {
+                if (lane == 0) {
+                    store_remote(&t.part_sums[part].m, __float_as_uint(a.m));
+                    store_remote(&t.part_sums[part].s, __float_as_uint(a.s));
+                    store_remote(&t.part_sums[part].u, __float_as_uint(a.u));
                 }
+                for (int i = lane; i < p.top; i += 32) store_remote(&t.list[Team<NT>::CAP + part * p.top + i], t.best[i]);
             }
-            if (part == 0 && p.top) {
+            __syncwarp();
+            cluster_arrive();
+            if (part) return;
+            cluster_wait();
+            if (warp == 0) {
+                a = t.part_sums[0];
+                for (int c = 1; c < p.parts; ++c) a = join(a, t.part_sums[c]);
+            }
+            if (p.top) {
                 const int n = p.parts * p.top;   // at most NT
-                if (id < n) t.list[id] = load_remote(&t.best[id % p.top], id / p.top);
+                if (id < n) t.list[id] = t.list[Team<NT>::CAP + id];
                 __syncthreads();
                 order<NT, NT>(t, n, p.top, id);
             }
-            __syncwarp();
-            cluster_sync();
         }
-        if (part || warp) return;
+        if (warp) return;
     }
     const float log2_s = log2f(a.s);
     if (lane == 0 && p.entropy) p.entropy[r] = (log2_s - a.u / a.s) * 0.6931471805599453f;
@@ -558,6 +558,7 @@ __global__ void __launch_bounds__(NT == 512 ? 512 : 256, NT == 512 ? 2 : 4)
 logprobs_held_kernel(const Params p) {
     constexpr int TEAMS = NT == 32 ? 8 : 1;
     __shared__ Team<NT> teams[TEAMS];
+    if (NT > 32 && p.parts > 1) cluster_arrive();   // see finish()
     grid_dependency_wait();
     grid_dependency_release();
     Team<NT>& t = teams[threadIdx.x / NT];
@@ -588,7 +589,7 @@ logprobs_held_kernel(const Params p) {
     Pairs sums;
     sums.raise(held);   // places without a vector are -inf
     sums.terms(held, mine0 < v1 ? (v1 - mine0 + NT - 1) / NT : 0);
-    finish<T, NT>(t, p, row, r, part, v0, v1, mine0 < v1, sums.all(), [&](bool reaches, float least) {
+    finish<T, NT, (NT > 32)>(t, p, row, r, part, v0, v1, mine0 < v1, sums.all(), [&](bool reaches, float least) {
         // eight lanes a share read it again, from the L1 or the L2
         for (uint32_t who = __ballot_sync(~0u, reaches); who;) {
             int from = -1;
@@ -613,20 +614,21 @@ constexpr int kStreamSmem = 2 * kAhead * 256 * 16;
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-template <class T>
+template <class T, bool SHARED>
 __global__ void __launch_bounds__(256, 4)
 logprobs_stream_kernel(const Params p) {
     constexpr int NT = 256, GROUP = kAhead * NT;
     __shared__ Team<NT> t;
     __shared__ __nv_bfloat16 tops[kBuckets][NT];
-    extern __shared__ uint4 ring[];   // [2][kAhead][NT]
+    extern __shared__ __align__(1024) uint4 ring[];   // [2][kAhead][NT]
     grid_dependency_wait();
     grid_dependency_release();
     const int id = threadIdx.x, lane = id & 31;
-    const int64_t r = blockIdx.x / p.parts;
-    const int part = blockIdx.x % p.parts;
+    const int parts = SHARED ? p.parts : 1;
+    const int64_t r = blockIdx.x / parts;
+    const int part = blockIdx.x % parts;
     const Row<T> row(static_cast<const T*>(p.x) + r * p.ld, p.classes);
-    const int v0 = (int)((int64_t)row.vectors * part / p.parts), v1 = (int)((int64_t)row.vectors * (part + 1) / p.parts);
+    const int v0 = (int)((int64_t)row.vectors * part / parts), v1 = (int)((int64_t)row.vectors * (part + 1) / parts);
     const int mine0 = v0 + id, end = min(v1, row.full1);
     // A thread's first vector, which may be partly outside the row, then whole groups of vectors, then what is left.
     auto groups_of = [&](int first) { return max(0, (end - first - 1) / GROUP); };
@@ -671,7 +673,8 @@ logprobs_stream_kernel(const Params p) {
     tops[kBuckets - 1][id] = __float2bfloat16_ru(others);
     asm volatile("cp.async.wait_all;" ::: "memory");
 
-    finish<T, NT>(t, p, row, r, part, v0, v1, mine0 < v1, sums.all(), [&](bool reaches, float least) {
+    if (SHARED && p.parts > 1) cluster_arrive();   // see finish()
+    finish<T, NT, SHARED>(t, p, row, r, part, v0, v1, mine0 < v1, sums.all(), [&](bool reaches, float least) {
         // share by share: a lane a bucket, then a lane a vector of those that reach it
         for (uint32_t who = __ballot_sync(~0u, reaches); who; who &= who - 1) {
             const int other = (id & ~31) + __ffs(who) - 1, first = v0 + other, n = groups_of(first);
@@ -701,8 +704,8 @@ sbnn_status launch_as(const Params& given, cudaStream_t st) {
     p.parts = 1;
     ChainedLaunchScope chained;
     // A warp a row: 64 x 1000 fp32 top 5 4.0 us (a CTA a row 4.3), 1000 x 1000 bf16 4.7 (10.2); but for many alternatives of few rows a CTA
-    // has the tighter bound: 64 x 1000 top 20 6.7 (4.7).
-    if (vectors <= 32 * kHeld && (p.top <= 8 || p.rows > 2 * sms)) {
+    // has the tighter bound, as long as none of the groups that it takes has nothing: 64 x 1000 top 20 6.7 (4.7).
+    if (vectors <= 32 * kHeld && (p.top <= 8 || p.rows > 2 * sms || vectors < 4 * p.top)) {
         SBNN_CUDA_TRY(launch_kernel(logprobs_held_kernel<T, 32>, dim3((unsigned)((p.rows + 7ll) / 8)), dim3(256), 0, st, p));
         return SBNN_OK;
     }
@@ -718,9 +721,10 @@ sbnn_status launch_as(const Params& given, cudaStream_t st) {
     } else if (share <= 512 * kHeld && (int64_t)p.rows * p.parts <= 2 * sms) {
         SBNN_CUDA_TRY(launch_kernel_cluster(logprobs_held_kernel<T, 512>, grid, dim3(512), 0, st, (unsigned)p.parts, p));
     } else {
-        const sbnn_status r = set_max_dyn_smem(reinterpret_cast<const void*>(&logprobs_stream_kernel<T>), kStreamSmem);
+        auto* const kernel = p.parts > 1 ? logprobs_stream_kernel<T, true> : logprobs_stream_kernel<T, false>;
+        const sbnn_status r = set_max_dyn_smem(reinterpret_cast<const void*>(kernel), kStreamSmem);
         if (r != SBNN_OK) return r;
-        SBNN_CUDA_TRY(launch_kernel_cluster(logprobs_stream_kernel<T>, grid, dim3(256), (size_t)kStreamSmem, st, (unsigned)p.parts, p));
+        SBNN_CUDA_TRY(launch_kernel_cluster(kernel, grid, dim3(256), (size_t)kStreamSmem, st, (unsigned)p.parts, p));
     }
     return SBNN_OK;
 }
