@@ -60,20 +60,27 @@ struct Shared {
     int abort;
 };
 
+// Pixels of a tile that each CTA of a cluster finishes: a multiple of 4.
+__host__ __device__ constexpr int exchange_width(int bn, int split) { return (bn + 4 * split - 1) / (4 * split) * 4; }
+
 // What a launch needs of shared memory, by parts (all multiples of 1024 bytes except the last).
 struct Layout {
     int a, b, sfa, sfb;     // a stage's operands; FUSED: b and sfb are those of one step and all steps of the CTA stay
-    int stage, resident, total;
+    int stage, resident;
+    int exchange;           // what the CTAs of a cluster send each other
+    int total;
 };
-__host__ __device__ inline Layout layout_of(int bn, int stages, int steps, bool fused) {
+__host__ __device__ inline Layout layout_of(int bn, int stages, int steps, int split, bool fused) {
+    const int own = (steps + split - 1) / split;
     Layout l;
     l.a = kABytes;
     l.b = bn * 128;
     l.sfa = 1024;
     l.sfb = 1024 * ((bn + 127) / 128);
     l.stage = l.a + l.sfa + (fused ? 0 : l.b + l.sfb);
-    l.resident = fused ? steps * (l.b + l.sfb) : 0;
-    l.total = stages * l.stage + l.resident + 1024 + (int)sizeof(Shared);
+    l.resident = fused ? own * (l.b + l.sfb) : 0;
+    l.exchange = split > 1 ? split * exchange_width(bn, split) * 512 : 0;
+    l.total = stages * l.stage + l.resident + l.exchange + 1024 + (int)sizeof(Shared);
     return l;
 }
 // Columns of tensor memory: sums, then the scales of the stages.
@@ -100,9 +107,6 @@ __device__ __forceinline__ void scales_to_tmem(uint32_t tmem, uint64_t d) {
 __device__ __forceinline__ void store_remote(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-
-// Pixels of a tile that each CTA of a cluster finishes: a multiple of 4.
-__host__ __device__ constexpr int exchange_width(int bn, int split) { return (bn + 4 * split - 1) / (4 * split) * 4; }
 
 // Polls without regard to the abort flag, a bounded number of times: what is in flight when a CTA gives up has to land first.
 __device__ __forceinline__ void land(uint64_t* bar, uint32_t parity) {
@@ -206,9 +210,10 @@ __global__ void __launch_bounds__(kThreads, 2)
 conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const Args a) {
     extern __shared__ uint8_t raw[];
     uint8_t* const base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-    const Layout l = layout_of(a.bn, a.stages, (a.steps + a.split - 1) / a.split, FUSED);
+    const Layout l = layout_of(a.bn, a.stages, a.steps, a.split, FUSED);
     uint8_t* const resident = base + a.stages * l.stage;
-    Shared& sh = *reinterpret_cast<Shared*>(resident + l.resident);
+    uint8_t* const exchange = resident + l.resident;
+    Shared& sh = *reinterpret_cast<Shared*>(exchange + l.exchange);
     // operands first, scales behind them: the operands of every stage start on 1024 bytes
     uint8_t* const scales = base + a.stages * (l.a + (FUSED ? 0 : l.b));
     const int op_stage = l.a + (FUSED ? 0 : l.b), sf_stage = l.sfa + (FUSED ? 0 : l.sfb);
@@ -237,6 +242,7 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         prefetch_map(&wmap);
         if (!FUSED) prefetch_map(&xmap);
     }
+    if (a.split > 1) cluster_arrive();   // waited for before the first store into another CTA's memory: all of the cluster have begun by then
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -349,13 +355,11 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     if (a.split == 1) {
         if (ok) drain(out, lanes, c0, c1);
     } else {
-        // Every CTA of the cluster is done with its stages: their memory takes the sums that the others send, four pixels of a
-        // channel at a time.  CTA r finishes pixels [r * width, (r + 1) * width).
-        cluster_sync();
+        // The CTAs send each other their sums, four pixels of a channel at a time; CTA r finishes pixels [r * width, (r + 1) * width).
+        cluster_wait();
         const int width = exchange_width(a.bn, a.split);
-        const float4* const exchange = reinterpret_cast<const float4*>(base);
         if (ok) {
-            const uint32_t ex = smem_u32(base);
+            const uint32_t ex = smem_u32(exchange);
             int owner = c0 / width, first_of_owner = owner * width;
             for (int c = c0; c < c1; c += 8) {
                 uint32_t v[8];
@@ -370,12 +374,14 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             }
         }
         __syncwarp();
-        cluster_sync();
+        cluster_arrive();
+        cluster_wait();
         if (ok) {
+            const float4* const sent = reinterpret_cast<const float4*>(exchange);
             for (int c = warp < 4 ? 0 : 4; c < width && rank * width + c < out.pixels; c += 8) {
                 float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
                 for (int r = 0; r < a.split; ++r) {
-                    const float4 g = exchange[(r * width + c) / 4 * 128 + row];
+                    const float4 g = sent[(r * width + c) / 4 * 128 + row];
                     f.x += g.x, f.y += g.y, f.z += g.z, f.w += g.w;
                 }
                 const uint32_t v[4] = {__float_as_uint(f.x), __float_as_uint(f.y), __float_as_uint(f.z), __float_as_uint(f.w)};
@@ -433,14 +439,13 @@ Plan plan_for(int64_t M, int Cout, int K, bool raw, int y_bytes) {
         for (int pass = 0; pass < 3 && best == 1e30; ++pass) {
             p.fused = raw && pass < 2;
             for (int split = 1; split <= 8 && split <= steps && (pass || split == 1 || ctiles * split <= 2 * sms); ++split) {
-                const int own = (steps + split - 1) / split;
                 const bool two = ctiles * split > sms && !pass;
                 const auto stages_in = [&](bool fused) {
                     int n = 6;
-                    while (n > 0 && layout_of(p.bn, n, own, fused).total > (two ? kHalfSmem : kMaxSmem)) --n;
+                    while (n > 0 && layout_of(p.bn, n, steps, split, fused).total > (two ? kHalfSmem : kMaxSmem)) --n;
                     return n;
                 };
-                if (stages_in(pass < 2) < (two ? 4 : 2)) continue;
+                if (stages_in(pass < 2) < (two ? 3 : 2)) continue;
                 const double us = few_us(ctiles, steps, split, (int)M, sms);
                 if (us < best) best = us, p.split = split, p.stages = stages_in(p.fused);
             }
@@ -450,12 +455,13 @@ Plan plan_for(int64_t M, int Cout, int K, bool raw, int y_bytes) {
     for (int bn = 64; bn <= 256; bn *= 2) {
         const int64_t tiles = ctiles * ((M + bn - 1) / bn);
         for (int split = 1; split <= 8 && split <= steps && (split == 1 || tiles * split <= sms); ++split) {
+            int stages = bn <= 128 ? 6 : 4;
+            while (stages > 1 && layout_of(bn, stages, steps, split, false).total > kMaxSmem) --stages;
             const double us = single_us(tiles, steps, bn, split, sms);
-            if (us < best) best = us, p.bn = bn, p.split = split;
+            if (stages >= 3 && us < best) best = us, p.bn = bn, p.split = split, p.stages = stages;
         }
     }
     p.pair = pair_us(M, Cout, steps, y_bytes, sms) < best;
-    p.stages = p.bn <= 128 ? 6 : 4;
     return p;
 }
 
@@ -486,7 +492,7 @@ sbnn_status launch(const Args& given, const Plan& p, const uint8_t* w_codes, con
                          : a.y_type == SBNN_F16 ? (p.fused ? conv_mxfp4_kernel<true, __half> : conv_mxfp4_kernel<false, __half>)
                                                 : (p.fused ? conv_mxfp4_kernel<true, __nv_bfloat16> : conv_mxfp4_kernel<false, __nv_bfloat16>);
     if ((r = set_max_dyn_smem(reinterpret_cast<const void*>(kernel), kMaxSmem)) != SBNN_OK) return r;
-    const size_t smem = (size_t)layout_of(a.bn, a.stages, (a.steps + a.split - 1) / a.split, p.fused).total;
+    const size_t smem = (size_t)layout_of(a.bn, a.stages, a.steps, a.split, p.fused).total;
     ChainedLaunchScope chained;   // the set-up overlaps the end of the launch before
     SBNN_CUDA_TRY(launch_kernel_cluster(kernel, dim3((unsigned)ctas), dim3(kThreads), smem, st, (unsigned)a.split, wmap, xmap, a));
     return SBNN_OK;
