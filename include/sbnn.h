@@ -484,8 +484,9 @@ SBNN_API sbnn_status sbnn_mxfp4_dequantize(const uint8_t* codes_dev, const uint8
  *   y_dev                      [M] rows of Cout elements of y_type, ldy apart
  *   flags                      SBNN_RELU or 0
  *   workspace_dev              device memory for the rounded activations, the two sizes of sbnn_mxfp4_bytes(M, Cin) added; of
- *                              the caller, so that calls in flight at the same time, and graphs, can have their own.  Not used,
- *                              and may be NULL, for M <= SBNN_MXFP4_DIRECT_ROWS and Cin <= SBNN_MXFP4_DIRECT_CHANNELS.
+ *                              the caller, so that calls in flight at the same time, and graphs, can have their own.  May be NULL
+ *                              for M <= SBNN_MXFP4_DIRECT_ROWS and Cin <= SBNN_MXFP4_DIRECT_CHANNELS (some such calls are
+ *                              quicker with it; results are the same bits).
  * sbnn_conv1x1_mxfp4_q takes activations that are in 4-bit form already (several layers on the same activations round them once).
  * A pixel's result does not depend on other pixels' values; the order of its sums depends on M, Cin and Cout alone.  A NaN block
  * makes every output that it meets NaN (0 after ReLU, as max(NaN, 0) is everywhere in this library).

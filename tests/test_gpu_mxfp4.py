@@ -235,6 +235,25 @@ def test_a_pixel_is_the_same_in_every_place_and_both_entries():
         assert np.array_equal(got[0], np.broadcast_to(got[0][:1], got[0].shape)) and np.array_equal(got[0], got[1])
 
 
+@pytest.mark.parametrize("m,k,n", [(32, 8192, 300), (5, 512, 130), (32, 2000, 19200)])
+def test_a_workspace_changes_no_result(m, k, n):
+    """Few pixels are rounded by a launch ahead where there is room and that is quicker."""
+    g = torch.Generator(device="cuda").manual_seed(k)
+    wc, ws = (torch.empty((b,), dtype=torch.uint8, device="cuda") for b in sbnn.mxfp4_bytes(n, k))
+    sbnn.mxfp4_quantize(torch.randn((n, k), generator=g, device="cuda"), k, wc, ws, n, k)
+    x = torch.randn((m, k), generator=g, device="cuda").half()
+    need = sum(sbnn.mxfp4_bytes(m, k))
+    got = []
+    for size in (None, need - 1, need):
+        y = torch.empty((m, n), device="cuda")
+        whole, work = guarded(size or 0)
+        sbnn.conv1x1_mxfp4(wc, ws, None, x, k, y, n, m, k, n, 0, work if size else None)
+        sbnn.get_async_status()
+        intact(whole)
+        got.append(y)
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
 def test_results_repeat_bit_by_bit():
     for m, k, n in ((1, 4096, 512), (20, 2048, 1000), (200, 1024, 300)):
         a, b = (layer(m, k, n, "f32", 16)[0] for _ in range(2))
