@@ -468,7 +468,7 @@ Plan plan_for(int64_t M, int Cout, int K, bool raw, int y_bytes) {
 sbnn_status launch(const Args& given, const Plan& p, const uint8_t* w_codes, const uint8_t* x_codes, cudaStream_t st) {
     if (p.pair) {
         const MxProduct q = {w_codes, given.w_scales, x_codes, given.x_scales, given.bias, given.y, given.ldy, given.y_type, given.M, given.Cout, given.K,
-                             given.relu};
+                             given.relu, given.early};
         return conv_mxfp4_pair(q, st);
     }
     Args a = given;

@@ -47,6 +47,7 @@ struct PairArgs {
     int M, Cout, K;
     int mtiles, ntiles;
     int relu, tiled_store;
+    int early;              // the launch before this one in the stream rounds the pixels and has seen the end of all before it
     int* status;
 };
 
@@ -162,10 +163,24 @@ conv_mxfp4_pair_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_co
     const uint32_t tmem = sh.tmem;
     volatile int* const abort = &sh.abort;
     grid_dependency_release();
-    grid_dependency_wait();
+    if (warp || !a.early) grid_dependency_wait();
 
     if (warp == 0) {
         if (lane == 0) {
+            // Channels do not depend on the launch that rounds the pixels (early): those of the first stages are on their way while it
+            // still runs.
+            const int ahead = a.early ? min(kStages, steps) : 0;
+            if (ahead) {
+                int mt, nt;
+                tile_at(a, pair, mt, nt);
+                for (int i = 0; i < ahead; ++i) {
+                    const uint32_t bar = remote_address(smem_u32(&sh.full[i]), 0);
+                    if (rank == 0) mbar_arrive_expect_tx(&sh.full[i], 2 * kStage);
+                    pair_g2s(base + i * 2 * kOperand + kOperand, &wmap, i * 64, nt * 256 + rank * 128, bar);
+                    pair_g2s(scales + i * 3 * 1024 + 1024, &wsmap, i * 256, nt * 2, bar);
+                }
+                grid_dependency_wait();
+            }
             int s = 0, used = 0;
             uint32_t phase = 1;
             bool ok = true;
@@ -176,13 +191,15 @@ conv_mxfp4_pair_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_co
                     if (used == kStages && !(ok = pair_wait(&sh.empty[s], phase, abort, a.status))) break;
                     if (used < kStages) ++used;
                     const uint32_t bar = remote_address(smem_u32(&sh.full[s]), 0);
-                    if (rank == 0) mbar_arrive_expect_tx(&sh.full[s], 2 * kStage);
                     uint8_t* const op = base + s * 2 * kOperand;
                     uint8_t* const sf = scales + s * 3 * 1024;
+                    if (t != pair || i >= ahead) {
+                        if (rank == 0) mbar_arrive_expect_tx(&sh.full[s], 2 * kStage);
+                        pair_g2s(op + kOperand, &wmap, i * 64, nt * 256 + rank * 128, bar);
+                        pair_g2s(sf + 1024, &wsmap, i * 256, nt * 2, bar);
+                    }
                     pair_g2s(op, &xmap, i * 64, mt * 256 + rank * 128, bar);
-                    pair_g2s(op + kOperand, &wmap, i * 64, nt * 256 + rank * 128, bar);
                     pair_g2s(sf, &xsmap, i * 256, mt * 2 + rank, bar);
-                    pair_g2s(sf + 1024, &wsmap, i * 256, nt * 2, bar);
                     if (++s == kStages) s = 0, phase ^= 1;
                 }
             }
@@ -333,7 +350,7 @@ sbnn_status conv_mxfp4_pair(const MxProduct& p, cudaStream_t st) {
     PairArgs a = {};
     sbnn_status r = async_status_word(&a.status);
     if (r != SBNN_OK) return r;
-    a.bias = p.bias, a.y = p.y, a.ldy = p.ldy, a.M = p.M, a.Cout = p.Cout, a.K = p.K, a.relu = p.relu;
+    a.bias = p.bias, a.y = p.y, a.ldy = p.ldy, a.M = p.M, a.Cout = p.Cout, a.K = p.K, a.relu = p.relu, a.early = p.early;
     a.mtiles = (int)(((int64_t)p.M + 255) / 256), a.ntiles = (int)(((int64_t)p.Cout + 255) / 256);
     const int size = p.y_type == SBNN_F32 ? 4 : 2, ktiles = mx_ktiles(p.K);
     if ((int64_t)a.mtiles * a.ntiles > 0x3fffffff) return fail(SBNN_ERR_SHAPE, "too many tiles");

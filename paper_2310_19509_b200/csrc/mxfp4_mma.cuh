@@ -16,6 +16,7 @@ struct MxProduct {
     void* y;
     int64_t ldy;
     int y_type, M, Cout, K, relu;
+    int early;   // it follows the launch that rounds the activations, which has seen the end of all before it
 };
 // conv_mxfp4_pair.cu: pairs of CTAs on 256 x 256 tiles.
 sbnn_status conv_mxfp4_pair(const MxProduct& p, cudaStream_t st);
