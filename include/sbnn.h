@@ -463,7 +463,8 @@ SBNN_API sbnn_status sbnn_head_noalloc(const sbnn_packed* fc, const float* x_dev
  * sbnn_mxfp4_bytes: the sizes of the two (host arithmetic only).
  * sbnn_mxfp4_quantize: x_dev [M] rows of K elements, ldx elements apart, to that form.
  * sbnn_mxfp4_dequantize: back, rounded to y's type; nothing is written behind a row's K elements.
- * Strides are in elements and any number from K up; all pointers are 16-byte aligned.  K at least 1; M = 0 returns SBNN_OK.
+ * Strides are in elements and any number from K up; all pointers are 16-byte aligned.  K from 1 to 2^30; M = 0 returns SBNN_OK.
+ * These entry points and those below refuse pointers that are not memory of the current device (SBNN_ERR_CUDA).
  * ------------------------------------------------------------------------------------------------ */
 enum { SBNN_F32 = 0, SBNN_F16 = 1, SBNN_BF16 = 2 }; /* element types of the entry points below */
 
@@ -488,6 +489,7 @@ SBNN_API sbnn_status sbnn_mxfp4_dequantize(const uint8_t* codes_dev, const uint8
  *                              for M <= SBNN_MXFP4_DIRECT_ROWS and Cin <= SBNN_MXFP4_DIRECT_CHANNELS (some such calls are
  *                              quicker with it; results are the same bits).
  * sbnn_conv1x1_mxfp4_q takes activations that are in 4-bit form already (several layers on the same activations round them once).
+ * M, Cin and Cout are at most 2^30.  Results below fp32's normal numbers may be lost.
  * A pixel's result does not depend on other pixels' values; the order of its sums depends on M, Cin and Cout alone.  A NaN block
  * makes every output that it meets NaN (0 after ReLU, as max(NaN, 0) is everywhere in this library).
  * Nothing is allocated or kept between calls.
@@ -513,7 +515,7 @@ SBNN_API sbnn_status sbnn_conv1x1_mxfp4_q(const uint8_t* w_codes_dev, const uint
  *                 lower index first, and their log probabilities.  Both may be NULL if top = 0.
  * Classes at -inf have probability 0 (log probability -inf).  Rows without a class above -inf, and rows with a logit of +inf or
  * NaN, have no distribution: their log probabilities and entropy are NaN.  Their most probable classes are still those
- * with the largest logits, where a NaN counts as -inf.  Sums are fp32.  One kernel; nothing is allocated.
+ * with the largest logits, where a NaN counts as -inf.  Sums are fp32.  classes is at most 2^30.  One kernel; nothing is allocated.
  */
 #define SBNN_LOGPROBS_MAX_TOP 32
 SBNN_API sbnn_status sbnn_logprobs(const void* logits_dev, int type, int64_t ld, int rows, int classes, const int32_t* targets_dev,

@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <string>
@@ -19,6 +20,10 @@ void clear_error();
 
 // SBNN_OK if the current device exists and is compute capability 10.x.
 sbnn_status check_device();
+
+// SBNN_OK if each of these (NULL ones apart) is memory that the current device can address as its own: device memory of it or managed
+// memory.  A host pointer, or memory of another device, would fault the kernel that is given it.
+sbnn_status check_device_memory(std::initializer_list<const void*> pointers);
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

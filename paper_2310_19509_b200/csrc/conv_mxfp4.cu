@@ -501,6 +501,7 @@ sbnn_status launch(const Args& given, const Plan& p, const uint8_t* w_codes, con
 sbnn_status check_call(const uint8_t* w_codes, const uint8_t* w_scales, const float* bias, const void* y, int y_type, int64_t ldy, int M, int Cin,
                        int Cout, int flags) {
     if (M < 0 || Cin <= 0 || Cout <= 0) return fail(SBNN_ERR_SHAPE, "bad shape M=%d Cin=%d Cout=%d", M, Cin, Cout);
+    if (M > 1 << 30 || Cin > 1 << 30 || Cout > 1 << 30) return fail(SBNN_ERR_UNSUPPORTED, "M=%d Cin=%d Cout=%d: 2^30 at most", M, Cin, Cout);
     if (y_type != SBNN_F32 && y_type != SBNN_F16 && y_type != SBNN_BF16) return fail(SBNN_ERR_UNSUPPORTED, "y_dev: unknown element type %d", y_type);
     if (ldy < Cout) return fail(SBNN_ERR_SHAPE, "y_dev: rows of %d elements do not fit a stride of %lld", Cout, (long long)ldy);
     if (flags & ~SBNN_RELU) return fail(SBNN_ERR_UNSUPPORTED, "unknown flag bits 0x%x", flags);
@@ -525,6 +526,7 @@ extern "C" sbnn_status sbnn_conv1x1_mxfp4_q(const uint8_t* w_codes_dev, const ui
     if (!aligned16(x_codes_dev) || !aligned16(x_scales_dev)) return fail(SBNN_ERR_ALIGN, "device pointers must be 16-byte aligned");
     if (M == 0) return SBNN_OK;
     if ((r = check_device()) != SBNN_OK) return r;
+    if ((r = check_device_memory({w_codes_dev, w_scales_dev, bias_dev, x_codes_dev, x_scales_dev, y_dev})) != SBNN_OK) return r;
     Args a = {};
     a.w_scales = w_scales_dev, a.x_scales = x_scales_dev, a.bias = bias_dev, a.y = y_dev, a.ldy = ldy, a.y_type = y_type;
     a.M = M, a.Cout = Cout, a.K = Cin, a.relu = flags & SBNN_RELU;
@@ -550,6 +552,7 @@ extern "C" sbnn_status sbnn_conv1x1_mxfp4(const uint8_t* w_codes_dev, const uint
     }
     if (M == 0) return SBNN_OK;
     if ((r = check_device()) != SBNN_OK) return r;
+    if ((r = check_device_memory({w_codes_dev, w_scales_dev, bias_dev, x_dev, y_dev, workspace_dev})) != SBNN_OK) return r;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     Args a = {};
     a.w_scales = w_scales_dev, a.bias = bias_dev, a.y = y_dev, a.ldy = ldy, a.y_type = y_type;

@@ -751,8 +751,9 @@ extern "C" sbnn_status sbnn_logprobs(const void* logits_dev, int type, int64_t l
         !aligned16(top_logprob_dev))
         return fail(SBNN_ERR_ALIGN, "device pointers must be 16-byte aligned");
     if (rows == 0) return SBNN_OK;
-    const sbnn_status r = check_device();
+    sbnn_status r = check_device();
     if (r != SBNN_OK) return r;
+    if ((r = check_device_memory({logits_dev, targets_dev, logprob_dev, entropy_dev, top_index_dev, top_logprob_dev})) != SBNN_OK) return r;
     Params p = {};
     p.x = logits_dev, p.targets = targets_dev, p.logprob = logprob_dev, p.entropy = entropy_dev;
     p.top_index = top_index_dev, p.top_logprob = top_logprob_dev;

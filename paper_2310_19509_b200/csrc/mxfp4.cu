@@ -152,6 +152,7 @@ bool whole_vectors(const void* p, int64_t ld, int K, int elem_bytes) { return al
 
 sbnn_status check_matrix(const char* what, const void* p, int type, int64_t ld, int M, int K) {
     if (M < 0 || K <= 0) return fail(SBNN_ERR_SHAPE, "bad shape M=%d K=%d", M, K);
+    if (K > 1 << 30) return fail(SBNN_ERR_UNSUPPORTED, "K=%d: 2^30 at most", K);
     if (type != SBNN_F32 && type != SBNN_F16 && type != SBNN_BF16) return fail(SBNN_ERR_UNSUPPORTED, "%s: unknown element type %d", what, type);
     if (ld < K) return fail(SBNN_ERR_SHAPE, "%s: rows of %d elements do not fit a stride of %lld", what, K, (long long)ld);
     if (!aligned16(p)) return fail(SBNN_ERR_ALIGN, "%s must be 16-byte aligned", what);
@@ -226,7 +227,7 @@ extern "C" sbnn_status sbnn_mxfp4_quantize(const void* x_dev, int x_type, int64_
     if (r != SBNN_OK) return r;
     if (!aligned16(codes_dev) || !aligned16(scales_dev)) return fail(SBNN_ERR_ALIGN, "codes_dev and scales_dev must be 16-byte aligned");
     if (M == 0) return SBNN_OK;
-    if ((r = check_device()) != SBNN_OK) return r;
+    if ((r = check_device()) != SBNN_OK || (r = check_device_memory({x_dev, codes_dev, scales_dev})) != SBNN_OK) return r;
     return mxfp4_quantize_launch(x_dev, x_type, ldx, codes_dev, scales_dev, M, K, static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -238,7 +239,7 @@ extern "C" sbnn_status sbnn_mxfp4_dequantize(const uint8_t* codes_dev, const uin
     if (r != SBNN_OK) return r;
     if (!aligned16(codes_dev) || !aligned16(scales_dev)) return fail(SBNN_ERR_ALIGN, "codes_dev and scales_dev must be 16-byte aligned");
     if (M == 0) return SBNN_OK;
-    if ((r = check_device()) != SBNN_OK) return r;
+    if ((r = check_device()) != SBNN_OK || (r = check_device_memory({codes_dev, scales_dev, y_dev})) != SBNN_OK) return r;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     switch (y_type) {
         case SBNN_F32: return dequantize_as<float>(codes_dev, scales_dev, y_dev, ldy, M, K, st);

@@ -25,6 +25,23 @@ sbnn_status fail(sbnn_status s, const char* fmt, ...) {
 
 void clear_error() { g_err[0] = 0; }
 
+sbnn_status check_device_memory(std::initializer_list<const void*> pointers) {
+    int dev = 0;
+    SBNN_CUDA_TRY(cudaGetDevice(&dev));
+    for (const void* p : pointers) {
+        if (!p) continue;
+        cudaPointerAttributes at = {};
+        if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
+            cudaGetLastError();
+            return fail(SBNN_ERR_CUDA, "%p is no device pointer", p);
+        }
+        if (at.type == cudaMemoryTypeManaged) continue;
+        if (at.type != cudaMemoryTypeDevice) return fail(SBNN_ERR_CUDA, "%p is host memory", p);
+        if (at.device != dev) return fail(SBNN_ERR_CUDA, "%p is memory of device %d, but device %d is current", p, at.device, dev);
+    }
+    return SBNN_OK;
+}
+
 sbnn_status check_device() {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);

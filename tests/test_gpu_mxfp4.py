@@ -1,4 +1,8 @@
 """4-bit quantisation and the 1x1 layer on 4-bit operands against their definition in 64 bits."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -9,6 +13,7 @@ from oracle import mxfp4 as O
 pytestmark = pytest.mark.gpu
 TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
 GUARD = 0xA5
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def guarded(nbytes, fill=GUARD):
@@ -267,6 +272,58 @@ def test_large_and_small_scales():
         x = activations(m, k, "f32", 17) * 2.0 ** ex
         check_layer(m, k, n, "f32", 17, x=x)
         check_layer(3, k, n, "f32", 17, x=x[:3])
+
+
+@pytest.mark.parametrize("m", [3, 40, 400])
+def test_blocks_of_zeros(m):
+    """Activations behind a ReLU: blocks, pixels and channels that are zero altogether have the scale 2^-127."""
+    x = activations(m, 416, "f32", 19).clamp(min=0)
+    x[:, 32:160] = 0
+    x[m // 2] = 0
+    x[0, 400:] = 2.0 ** -126
+    check_layer(m, 416, 260, "f32", 19, x=x, relu=True)
+
+
+def test_memory_that_is_not_the_devices_is_refused():
+    x, y = torch.zeros((2, 64)), torch.zeros((2, 64), device="cuda")
+    c, s = torch.zeros((64 * 32,), dtype=torch.uint8, device="cuda"), torch.zeros((512,), dtype=torch.uint8, device="cuda")
+    for call in (lambda: sbnn.mxfp4_quantize(x, 64, c, s, 2, 64), lambda: sbnn.mxfp4_dequantize(c.cpu(), s, y, 64, 2, 64),
+                 lambda: sbnn.conv1x1_mxfp4(c, s, None, y, 64, x, 64, 2, 64, 64, 0), lambda: sbnn.conv1x1_mxfp4_q(c, s, None, c, s.cpu(), y, 64, 2, 64, 64, 0),
+                 lambda: sbnn.logprobs(x, 64, 2, 64, None, 0, None, None, 0, None, None)):
+        with pytest.raises(sbnn.SbnnError) as e:
+            call()
+        assert e.value.name == "SBNN_ERR_CUDA" and "host memory" in e.value.detail
+    sbnn.get_async_status()
+
+
+def test_first_calls_of_a_process_can_be_captured():
+    """Nothing is set up by a call outside the capture: a new process records its first calls and replays them."""
+    code = """
+import torch, paper_2310_19509_b200 as sbnn
+x, w = torch.randn((40, 512), device="cuda").bfloat16(), torch.randn((300, 512), device="cuda").bfloat16()
+e = lambda n: torch.empty((n,), dtype=torch.uint8, device="cuda")
+wc, ws, work = *map(e, sbnn.mxfp4_bytes(300, 512)), e(sum(sbnn.mxfp4_bytes(40, 512)))
+y, z = torch.zeros((40, 300), device="cuda"), torch.zeros((3, 300), device="cuda")
+h, i, l = torch.zeros((40,), device="cuda"), torch.zeros((40, 3), dtype=torch.int32, device="cuda"), torch.zeros((40, 3), device="cuda")
+def calls():
+    sbnn.mxfp4_quantize(w, 512, wc, ws, 300, 512)
+    sbnn.conv1x1_mxfp4(wc, ws, None, x, 512, y, 300, 40, 512, 300, 0, work)
+    sbnn.conv1x1_mxfp4(wc, ws, None, x, 512, z, 300, 3, 512, 300, 0)
+    sbnn.logprobs(y, 300, 40, 300, None, 0, None, h, 3, i, l)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    calls()
+g.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (y, z, h, i, l)]
+calls()
+sbnn.get_async_status()
+assert all(torch.equal(a, b) for a, b in zip(got, (y, z, h, i, l))) and float(y.abs().sum()) > 0
+print("replayed")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT, timeout=300)
+    assert r.returncode == 0 and "replayed" in r.stdout, r.stderr[-2000:]
 
 
 def test_side_stream_and_graph():

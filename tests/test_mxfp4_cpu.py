@@ -63,6 +63,7 @@ def test_quantize_refusals(call):
     assert run(x=T(at=0)) == run(codes=None) == run(scales=None) == "SBNN_ERR_NULL"
     assert run(m=-1) == run(k=0) == run(ld=63) == "SBNN_ERR_SHAPE"
     assert run(x=T(at=P + 4)) == run(codes=P + 1) == run(scales=P + 8) == "SBNN_ERR_ALIGN"
+    assert run(k=2 ** 30 + 1, ld=2 ** 31) == "SBNN_ERR_UNSUPPORTED"
     with pytest.raises(TypeError):
         run(x=T("float64"))
     fn(*((T(), 64, P, P, 0, 64) if call == "quantize" else (P, P, T(), 64, 0, 64)), stream=0)      # no rows: nothing to do
@@ -90,7 +91,7 @@ def test_conv_q_refusals():
 
     assert run(w=None) == run(ws=None) == run(x=None) == run(xs=None) == run(y=T(at=0)) == "SBNN_ERR_NULL"
     assert run(m=-1) == run(cin=0) == run(cout=-3) == run(ldy=47) == "SBNN_ERR_SHAPE"
-    assert run(flags=sbnn.SBNN_OUT_CM) == "SBNN_ERR_UNSUPPORTED"
+    assert run(flags=sbnn.SBNN_OUT_CM) == run(m=2 ** 30 + 1) == run(cin=2 ** 30 + 1) == run(cout=2 ** 30 + 1, ldy=2 ** 31) == "SBNN_ERR_UNSUPPORTED"
     assert run(x=P + 8) == run(xs=P + 4) == "SBNN_ERR_ALIGN"
 
 
