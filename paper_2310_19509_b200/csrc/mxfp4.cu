@@ -32,12 +32,13 @@ quantize_kernel(const T* __restrict__ x, int64_t ldx, uint8_t* __restrict__ code
     const int rows = (int)min((int64_t)ROWS, M - row0), k0 = kt * 128;
     const int64_t ldc = 16 * (int64_t)mx_blocks(K);
     const bool word = ((k0 + l * 8) & ~31) < K;   // the lane's word of codes exists
-    const int first = warp * kRows;
+    // addresses by addition: built anew for each row they were a third of the instructions, and those are what bounds bf16
+    const int r0 = warp * kRows + at;
+    const T* p = x + (row0 + r0) * ldx + k0;
     Eight<T> e[BATCH];   // VEC: channels k0 + 8 l ..; else channel k0 + l + LPR j
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
-        const int r = first + i * AT + at;
-        const T* p = x + (row0 + r) * ldx + k0;
+    for (int i = 0; i < BATCH; ++i, p += AT * ldx) {
+        const int r = r0 + i * AT;
         if (VEC) {
             if (r < rows && k0 + l * 8 < K) {
                 load8<true>(e[i], p + l * 8, 8);
@@ -50,9 +51,10 @@ quantize_kernel(const T* __restrict__ x, int64_t ldx, uint8_t* __restrict__ code
             for (int j = 0; j < 8; ++j) e[i].v[j] = r < rows && k0 + l + LPR * j < K ? __ldg(p + l + LPR * j) : from_float<T>(0.f);
         }
     }
+    uint8_t* to = codes + (row0 + r0) * ldc + (k0 >> 1) + l * 4;
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
-        const int r = first + i * AT + at;
+    for (int i = 0; i < BATCH; ++i, to += AT * ldc) {
+        const int r = r0 + i * AT;
         if (!VEC) {
             Eight<T>* const row = turn + (threadIdx.x - l);
             __syncwarp();
@@ -69,7 +71,7 @@ quantize_kernel(const T* __restrict__ x, int64_t ldx, uint8_t* __restrict__ code
         uint32_t w = byte << 8 * (l >> 2 & 3);
         w |= __shfl_xor_sync(~0u, w, 4);
         if (LPR > 8) w |= __shfl_xor_sync(~0u, w, 8);
-        if (r < rows && word) *reinterpret_cast<uint32_t*>(codes + (row0 + r) * ldc + (k0 >> 1) + l * 4) = c;
+        if (r < rows && word) *reinterpret_cast<uint32_t*>(to) = c;
         if ((l & 15) == 0) tile[l >> 4][r] = w;
     }
     // (stored by the warps as they have them, a word of two lanes a row: 16384 x 8192 bf16 74 us, like this 63)
@@ -92,22 +94,22 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
     const int rows = (int)min((int64_t)ROWS, M - row0), k0 = kt * 128;
     const int64_t ldc = 16 * (int64_t)mx_blocks(K);
     const bool word = ((k0 + l * 8) & ~31) < K;
-    const int first = warp * kRows;
-    if (first >= rows) return;
+    const int r0 = warp * kRows + at;
+    const uint8_t* from = codes + (row0 + r0) * ldc + (k0 >> 1) + l * 4;
+    const uint8_t* sf = scales + mx_scale_offset(row0 + r0, 4 * (kt + (l >> 4)), ktiles);   // the next row's is 16 bytes on: a CTA's rows share a tile
     uint32_t c[BATCH], s[BATCH];   // a word of codes, the scales of the four blocks that it is one of
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
-        const int r = first + i * AT + at;
+    for (int i = 0; i < BATCH; ++i, from += AT * ldc) {
         c[i] = s[i] = 0;
-        if (r < rows && word) {
-            c[i] = __ldg(reinterpret_cast<const uint32_t*>(codes + (row0 + r) * ldc + (k0 >> 1) + l * 4));
-            s[i] = __ldg(reinterpret_cast<const uint32_t*>(scales + mx_scale_offset(row0 + r, 4 * (kt + (l >> 4)), ktiles)));
+        if (r0 + i * AT < rows && word) {
+            c[i] = __ldg(reinterpret_cast<const uint32_t*>(from));
+            s[i] = __ldg(reinterpret_cast<const uint32_t*>(sf + i * AT * 16));
         }
     }
+    T* p = y + (row0 + r0) * ldy + k0;
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
-        const int r = first + i * AT + at;
-        T* p = y + (row0 + r) * ldy + k0;
+    for (int i = 0; i < BATCH; ++i, p += AT * ldy) {
+        const int r = r0 + i * AT;
         constexpr bool LINES = VEC && sizeof(T) == 4 && LPR == 32;
         float s0, s1;   // of the first and the last four of the lane's channels
         if (LINES) {
@@ -126,8 +128,7 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float2 f = __half22float2(h[j]);
-            e.v[2 * j] = from_float<T>(f.x * (j < 2 ? s0 : s1));
-            e.v[2 * j + 1] = from_float<T>(f.y * (j < 2 ? s0 : s1));
+            put2(e, 2 * j, f.x * (j < 2 ? s0 : s1), f.y * (j < 2 ? s0 : s1));
         }
         if (LINES) {
             const float4* const f = reinterpret_cast<const float4*>(e.v);

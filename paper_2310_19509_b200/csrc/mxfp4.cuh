@@ -108,6 +108,12 @@ __device__ __forceinline__ void store8(const Eight<T>& e, T* p, int n) {
             if (i < n) p[i] = e.v[i];
     }
 }
+// Two values into places i and i + 1.
+__device__ __forceinline__ void put2(Eight<float>& e, int i, float a, float b) { e.v[i] = a, e.v[i + 1] = b; }
+__device__ __forceinline__ void put2(Eight<__half>& e, int i, float a, float b) { *reinterpret_cast<__half2*>(e.v + i) = __floats2half2_rn(a, b); }
+__device__ __forceinline__ void put2(Eight<__nv_bfloat16>& e, int i, float a, float b) {
+    *reinterpret_cast<__nv_bfloat162*>(e.v + i) = __floats2bfloat162_rn(a, b);
+}
 // Bits of the largest magnitude of the eight, as fp32.  Magnitudes are compared by their bits, which puts infinities and NaN
 // on top.
 template <class T>
@@ -133,8 +139,9 @@ __device__ __forceinline__ uint32_t encode8(const Eight<T>& e, uint32_t byte) {
     const float inv = mx_inverse_scale(byte);
     float f[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = byte == 255u ? 0.f : to_float(e.v[i]) * inv;
-    return mx_encode8(f);
+    for (int i = 0; i < 8; ++i) f[i] = to_float(e.v[i]) * inv;
+    const uint32_t codes = mx_encode8(f);
+    return byte == 255u ? 0u : codes;
 }
 
 }  // namespace sbnn
