@@ -40,17 +40,6 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-    f32x2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-    f32x2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 // Order of values: larger keys first.  -0 equals 0, NaN counts as -inf, 0 is below every value.
 __device__ __forceinline__ uint32_t key_of(float v) {
     if (v != v) v = -INFINITY;
@@ -170,14 +159,12 @@ __device__ __forceinline__ float element(const Vec<T>& q, int e) {
 // A thread's sums, in pairs.
 struct Pairs {
     float m;
-    f32x2 s, u;
-    __device__ Pairs() : m(-INFINITY), s(0), u(0) {}
-    __device__ __forceinline__ void term(f32x2 t) {
-        float t0, t1;
-        unpack2(t, t0, t1);
-        const f32x2 e = pack2(exp2_of(t0), exp2_of(t1));
-        s = add2(s, e);
-        fma2(u, e, t);
+    float2 s, u;
+    __device__ Pairs() : m(-INFINITY), s(make_float2(0.f, 0.f)), u(make_float2(0.f, 0.f)) {}
+    __device__ __forceinline__ void term(float2 t) {
+        const float2 e = make_float2(exp2_of(t.x), exp2_of(t.y));
+        s = __fadd2_rn(s, e);
+        u = __ffma2_rn(e, t, u);
     }
     // The base for these, whose largest is returned, and what they add.
     template <class T, int V>
@@ -187,9 +174,8 @@ struct Pairs {
         for (int i = 1; i < V; ++i) most = fmaxf(most, largest(q[i]));
         if (most > m) {
             const float d = shift(m, most), e = exp2_of(d);
-            fma2(u, dup2(d), s);
-            u = mul2(u, dup2(e));
-            s = mul2(s, dup2(e));
+            u = __fmul2_rn(__ffma2_rn(make_float2(d, d), s, u), make_float2(e, e));
+            s = __fmul2_rn(s, make_float2(e, e));
             m = most;
         }
         return most;
@@ -198,16 +184,15 @@ struct Pairs {
     template <class T, int V>
     __device__ __forceinline__ void terms(Vec<T> (&q)[V], int there) {
         if (m > Least<T>::kFast && m <= kHuge) {
-            const f32x2 scale = dup2(kLog2E), base = dup2(-__fmul_rn(m, kLog2E));
+            const float b = -__fmul_rn(m, kLog2E);
+            const float2 scale = make_float2(kLog2E, kLog2E), base = make_float2(b, b);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 if (i >= there) break;
                 Least<T>::clamp(q[i]);
 #pragma unroll
                 for (int j = 0; j < Vec<T>::N; j += 2) {
-                    f32x2 t = base;
-                    fma2(t, pack2(to_float(q[i].v[j]), to_float(q[i].v[j + 1])), scale);
-                    term(t);
+                    term(__ffma2_rn(make_float2(to_float(q[i].v[j]), to_float(q[i].v[j + 1])), scale, base));
                 }
             }
         } else {   // rare, and little code: see take()
@@ -217,7 +202,7 @@ struct Pairs {
             for (int i = 0; i < V; ++i)
 #pragma unroll 1
                 for (int j = 0; i < there && j < Vec<T>::N; j += 2)
-                    term(pack2(max_nan(fmaf(element(q[i], j) - from, kLog2E, base), kFar), max_nan(fmaf(element(q[i], j + 1) - from, kLog2E, base), kFar)));
+                    term(make_float2(max_nan(fmaf(element(q[i], j) - from, kLog2E, base), kFar), max_nan(fmaf(element(q[i], j + 1) - from, kLog2E, base), kFar)));
         }
     }
     template <class T, int V>
@@ -231,10 +216,7 @@ struct Pairs {
         add(one);
     }
     __device__ __forceinline__ Sums all() const {
-        float a, b, c, d;
-        unpack2(s, a, b);
-        unpack2(u, c, d);
-        return {m, a + b, c + d};
+        return {m, s.x + s.y, u.x + u.y};
     }
 };
 
