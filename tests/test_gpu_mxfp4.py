@@ -357,6 +357,48 @@ def test_side_stream_and_graph():
         assert torch.equal(y[0], want[a]) and torch.equal(y[1], want[b])
 
 
+def test_capture_behind_copies_and_joined_streams():
+    """Calls captured behind copies, and behind two streams that join, start when all of that is done."""
+    m, k, n = 64, 512, 300
+    g = torch.Generator(device="cuda").manual_seed(5)
+    w = [torch.randn((n, k), generator=g, device="cuda") for _ in range(3)]
+    xs = [torch.randn((m, k), generator=g, device="cuda") for _ in range(3)]
+    x, wd, y = torch.zeros_like(xs[0]), torch.zeros_like(w[0]), torch.zeros((m, n), device="cuda")
+    wc, ws = (torch.empty((b,), dtype=torch.uint8, device="cuda") for b in sbnn.mxfp4_bytes(n, k))
+    work = torch.empty((sum(sbnn.mxfp4_bytes(m, k)),), dtype=torch.uint8, device="cuda")
+    h, ti, tl = torch.empty((m,), device="cuda"), torch.empty((m, 4), dtype=torch.int32, device="cuda"), torch.empty((m, 4), device="cuda")
+    x_in, w_in = torch.zeros_like(x), torch.zeros_like(wd)
+    side = torch.cuda.Stream()
+
+    def calls():
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        x.copy_(x_in)
+        with torch.cuda.stream(side):
+            wd.copy_(w_in)
+            sbnn.mxfp4_quantize(wd, k, wc, ws, n, k)
+        here.wait_stream(side)
+        sbnn.conv1x1_mxfp4(wc, ws, None, x, k, y, n, m, k, n, 0, work)
+        sbnn.logprobs(y, n, m, n, None, 0, None, h, 4, ti, tl)
+
+    want = []
+    for a, b in zip(xs, w):
+        x_in.copy_(a), w_in.copy_(b)
+        torch.cuda.synchronize()
+        calls()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in (y, h, ti, tl)])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for _ in range(5):
+        for a, b, expected in zip(xs, w, want):
+            x_in.copy_(a), w_in.copy_(b)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(p, q) for p, q in zip((y, h, ti, tl), expected))
+
+
 def test_offsets_past_32_bits():
     """The last rows of matrices of more than 2^31 elements."""
     m, k, ld = 70000, 32, 65536
