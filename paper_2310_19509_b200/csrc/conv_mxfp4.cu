@@ -243,6 +243,7 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         prefetch_map(&wmap);
         if (!FUSED) prefetch_map(&xmap);
     }
+    __syncwarp();
     if (a.split > 1) cluster_arrive();   // waited for before the first store into another CTA's memory: all of the cluster have begun by then
     tc_fence_before_sync();
     __syncthreads();
@@ -341,7 +342,7 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     }
     // All warps drain: two share a quarter of the lanes and halve the columns.
     __syncwarp();
-    const bool ok = mbar_wait(&sh.done, 0, abort, a.status, SBNN_ERR_TIMEOUT);
+    const bool ok = __all_sync(~0u, mbar_wait(&sh.done, 0, abort, a.status, SBNN_ERR_TIMEOUT));
     tc_fence_after_sync();
     const int row = (warp & 3) * 32 + lane, o = ct * 128 + row;
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
