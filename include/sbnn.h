@@ -490,8 +490,8 @@ SBNN_API sbnn_status sbnn_mxfp4_dequantize(const uint8_t* codes_dev, const uint8
  *                              quicker with it; results are the same bits).
  * sbnn_conv1x1_mxfp4_q takes activations that are in 4-bit form already (several layers on the same activations round them once).
  * M, Cin and Cout are at most 2^30.  Results below fp32's normal numbers may be lost.
- * A pixel's result does not depend on other pixels' values; the order of its sums depends on M, Cin and Cout alone.  A NaN block
- * makes every output that it meets NaN (0 after ReLU, as max(NaN, 0) is everywhere in this library).
+ * A pixel's result does not depend on other pixels' values; the order of its sums depends on M, Cin, Cout and y's type alone.
+ * A NaN block makes every output that it meets NaN (0 after ReLU, as max(NaN, 0) is everywhere in this library).
  * Nothing is allocated or kept between calls.
  */
 #define SBNN_MXFP4_DIRECT_ROWS 32
