@@ -293,6 +293,22 @@ __device__ __forceinline__ uint32_t bound_of(const Team<NT>& t, int top) {
         if (rank[h] < top) bound = min(bound, k[h]);
     return __reduce_min_sync(~0u, bound);
 }
+// Whole warp: the same of all the keys that its lanes have (0: none), the largest number that at least `top` reach, or one below it
+// that no more reach; 0 where fewer exist.
+template <int V>
+__device__ __forceinline__ uint32_t bound_of_all(const uint32_t (&keys)[V], int top) {
+    uint32_t bound = 0;
+#pragma unroll 1
+    for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+        int reach = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) reach += keys[i] >= (bound | bit);
+        reach = __reduce_add_sync(~0u, reach);
+        if (reach >= top) bound |= bit;
+        if (reach == top) break;
+    }
+    return bound;
+}
 // The classes of a vector that reach the bound, into the list as far as it goes.  (Little code, called from one place of a kernel: a row's
 // end runs it once a warp, and what is not in the instruction cache then is waited for.  Unrolled over the elements and at
 // several places it made the 20 most probable classes of 2048 x 131072 cost 61 us.)
@@ -439,9 +455,10 @@ __device__ __forceinline__ void store_remote(const void* p, unsigned long long v
 // What is left of a row, or of the part [v0, v1) of it that a CTA has, when every thread has its sums `a` (has: of at least one vector):
 // joins them, finds the most probable classes and, in the first part, writes the answers.  scan(reaches, least), called by whole warps,
 // takes what is least or more out of the shares of the threads that reach the bound.
+// tighter, of a warp: a better bound for many alternatives than that of its lanes' maxima, 0 without one.
 template <class T, int NT, bool SHARED, class Scan>
 __device__ __forceinline__ void finish(Team<NT>& t, const Params& p, const Row<T>& row, int64_t r, int part, int v0, int v1, bool has, Sums a,
-                                       Scan scan) {
+                                       uint32_t tighter, Scan scan) {
     constexpr int WARPS = Team<NT>::WARPS, GL = NT / Team<NT>::GROUPS;
     const int id = threadIdx.x % NT, lane = id & 31, warp = id >> 5;
     // the groups' maxima; from them the row's, to which everybody brings down its sums, and the bound
@@ -470,7 +487,7 @@ __device__ __forceinline__ void finish(Team<NT>& t, const Params& p, const Row<T
         __syncthreads();
     }
     if (p.top) {
-        const uint32_t bound = p.top == 1 ? most : NT == 32 ? bound_of<NT>(t, p.top) : t.bound;
+        const uint32_t bound = p.top == 1 ? most : NT > 32 ? t.bound : tighter ? tighter : bound_of<NT>(t, p.top);
         scan(mine >= bound && mine, bound ? value_of(bound) : -INFINITY);
         team_sync<NT>();
         int n = t.count;
@@ -536,7 +553,7 @@ __device__ __forceinline__ void finish(Team<NT>& t, const Params& p, const Row<T
 // Rows that the threads of a team hold (kHeld vectors a thread at most).  NT = 32: eight rows a CTA, a warp each; else a row, or
 // with parts > 1 one of the parts of a row that a cluster shares.
 template <class T, int NT>
-__global__ void __launch_bounds__(NT == 512 ? 512 : 256, NT == 512 ? 2 : 4)
+__global__ void __launch_bounds__(NT == 32 ? 256 : NT, NT == 512 ? 2 : NT == 128 ? 8 : 4)
 logprobs_held_kernel(const Params p) {
     constexpr int TEAMS = NT == 32 ? 8 : 1;
     __shared__ Team<NT> teams[TEAMS];
@@ -568,10 +585,20 @@ logprobs_held_kernel(const Params p) {
                 if (mine0 + i * NT == v) held[i] = q;
         }
     }
+    // Nearly as many alternatives as lanes: the bound comes from the vectors' maxima, of which there are more (1731 x 422 bf16, top 32,
+    // 45 us without and 15 with: the least of the lanes' maxima is reached by more classes than the list holds; 4 x 302, top 20, 5.6
+    // and 6.8).
+    uint32_t tighter = 0;
+    if (NT == 32 && p.top > 24 && v1 > 32) {
+        uint32_t keys[kHeld];
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) keys[i] = mine0 + i * NT < v1 ? key_of(largest(held[i])) : 0u;
+        tighter = bound_of_all(keys, p.top);
+    }
     Pairs sums;
     sums.raise(held);   // places without a vector are -inf
     sums.terms(held, mine0 < v1 ? (v1 - mine0 + NT - 1) / NT : 0);
-    finish<T, NT, (NT > 32)>(t, p, row, r, part, v0, v1, mine0 < v1, sums.all(), [&](bool reaches, float least) {
+    finish<T, NT, (NT > 32)>(t, p, row, r, part, v0, v1, mine0 < v1, sums.all(), tighter, [&](bool reaches, float least) {
         // eight lanes a share read it again, from the L1 or the L2
         for (uint32_t who = __ballot_sync(~0u, reaches); who;) {
             int from = -1;
@@ -656,7 +683,7 @@ logprobs_stream_kernel(const Params p) {
     asm volatile("cp.async.wait_all;" ::: "memory");
 
     if (SHARED && p.parts > 1) cluster_arrive();   // see finish()
-    finish<T, NT, SHARED>(t, p, row, r, part, v0, v1, mine0 < v1, sums.all(), [&](bool reaches, float least) {
+    finish<T, NT, SHARED>(t, p, row, r, part, v0, v1, mine0 < v1, sums.all(), 0u, [&](bool reaches, float least) {
         // share by share: a lane a bucket, then a lane a vector of those that reach it
         for (uint32_t who = __ballot_sync(~0u, reaches); who; who &= who - 1) {
             const int other = (id & ~31) + __ffs(who) - 1, first = v0 + other, n = groups_of(first);
@@ -698,7 +725,10 @@ sbnn_status launch_as(const Params& given, cudaStream_t st) {
     const dim3 grid((unsigned)(p.rows * p.parts));
     const int64_t share = (vectors + p.parts - 1) / p.parts;
     // 512 threads hold a share where all run at once: 200 x 32000 bf16 7.6 us (streamed 10.9), 3166 x 20000 47 (38)
-    if (share <= 256 * kHeld) {
+    // 128 threads a row where rows are more than the SMs hold of 256: 2169 x 1253 fp32, top 5, 10.1 us (17.6), 4000 x 3000 fp16 17.5 (32.3)
+    if (share <= 128 * kHeld && p.rows > 2 * sms) {
+        SBNN_CUDA_TRY(launch_kernel(logprobs_held_kernel<T, 128>, grid, dim3(128), 0, st, p));
+    } else if (share <= 256 * kHeld) {
         SBNN_CUDA_TRY(launch_kernel_cluster(logprobs_held_kernel<T, 256>, grid, dim3(256), 0, st, (unsigned)p.parts, p));
     } else if (share <= 512 * kHeld && (int64_t)p.rows * p.parts <= 2 * sms) {
         SBNN_CUDA_TRY(launch_kernel_cluster(logprobs_held_kernel<T, 512>, grid, dim3(512), 0, st, (unsigned)p.parts, p));

@@ -53,13 +53,14 @@ def logits(rows, v, dtype, seed=0, scale=2.5):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,v", [(1, 1), (3, 2), (2, 7), (5, 33), (4, 100), (64, 1000), (3, 1024), (2, 4099), (7, 8192), (5, 16500), (1, 50257),
-                                    (2, 131072), (200, 9001), (1300, 10), (1250, 1000), (1200, 2000)])
+                                    (2, 131072), (200, 9001), (1300, 10), (1250, 1000), (1200, 2000), (400, 1253),
+                                    (350, 4100), (300, 8100)])
 def test_sizes(rows, v, dtype):
     check(logits(rows, v, dtype, rows + v))
 
 
 @pytest.mark.parametrize("top", [0, 1, 2, 20, 31, 32])
-@pytest.mark.parametrize("rows,v", [(1300, 300), (3, 32), (3, 3000), (2, 40000), (300, 20000)])
+@pytest.mark.parametrize("rows,v", [(1300, 300), (700, 422), (4, 302), (3, 32), (3, 3000), (2, 40000), (300, 20000), (400, 2600)])
 def test_numbers_of_alternatives(rows, v, top):
     check(logits(rows, v, "bf16", top), top=top)
 
@@ -73,8 +74,8 @@ def test_strides(rows, v, ld, dtype):
     check(logits(rows, v, dtype, 3), ld=ld)
 
 
-# One size for every form a row is worked on in: by a warp (many rows), a CTA of 128, of 512, a cluster.
-SHAPES = [(1250, 600), (3, 1000), (300, 20000), (2, 70001)]
+# One size for every form a row is worked on in: by a warp, a cluster of CTAs that hold it, CTAs that stream it, that hold it.
+SHAPES = [(1250, 600), (3, 1000), (300, 20000), (2, 70001), (320, 3001)]
 
 
 @pytest.mark.parametrize("rows,v", SHAPES)
