@@ -127,7 +127,7 @@ __device__ __forceinline__ void round_blocks(const Args& a, uint8_t* b, uint8_t*
         const T* p = static_cast<const T*>(a.x) + row * a.ldx + k;
         if (VEC && n >= 32) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) load8<true>(e[u][q], p + 8 * q, 8);
+            for (int q = 0; q < 4; ++q) load8(e[u][q], p + 8 * q);
         } else {
 #pragma unroll
             for (int q = 0; q < 4; ++q)

@@ -42,7 +42,7 @@ quantize_kernel(const T* __restrict__ x, int64_t ldx, uint8_t* __restrict__ code
         const int r = r0 + i * AT;
         if (VEC) {
             if (r < rows && k0 + l * 8 < K) {
-                load8<true>(e[i], p + l * 8, 8);
+                load8(e[i], p + l * 8);
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) e[i].v[j] = from_float<T>(0.f);
@@ -136,7 +136,7 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
             if (r < rows && k0 + 4 * l < K) *reinterpret_cast<float4*>(p + 4 * l) = f[0];
             if (r < rows && k0 + 128 + 4 * l < K) *reinterpret_cast<float4*>(p + 128 + 4 * l) = f[1];
         } else if (VEC) {
-            if (r < rows && k0 + l * 8 < K) store8<true>(e, p + l * 8, 8);
+            if (r < rows && k0 + l * 8 < K) store8(e, p + l * 8);
         } else {
             Eight<T>* const row = turn + (threadIdx.x - l);
             __syncwarp();

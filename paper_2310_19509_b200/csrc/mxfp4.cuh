@@ -82,31 +82,20 @@ template <class T>
 struct Eight {
     alignas(16) T v[8];
 };
-// VEC: `p` is 16-byte aligned and all eight are there; else `n` of them are (the others read as zero).
-template <bool VEC, class T>
-__device__ __forceinline__ void load8(Eight<T>& e, const T* p, int n) {
-    if (VEC) {
-        const uint4* q = reinterpret_cast<const uint4*>(p);
-        uint4* d = reinterpret_cast<uint4*>(e.v);
+// From and to 16-byte aligned memory.
+template <class T>
+__device__ __forceinline__ void load8(Eight<T>& e, const T* p) {
+    const uint4* q = reinterpret_cast<const uint4*>(p);
+    uint4* d = reinterpret_cast<uint4*>(e.v);
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(T) * 8 / 16); ++i) d[i] = __ldg(q + i);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e.v[i] = i < n ? __ldg(p + i) : from_float<T>(0.f);
-    }
+    for (int i = 0; i < (int)(sizeof(T) * 8 / 16); ++i) d[i] = __ldg(q + i);
 }
-template <bool VEC, class T>
-__device__ __forceinline__ void store8(const Eight<T>& e, T* p, int n) {
-    if (VEC) {
-        uint4* q = reinterpret_cast<uint4*>(p);
-        const uint4* d = reinterpret_cast<const uint4*>(e.v);
+template <class T>
+__device__ __forceinline__ void store8(const Eight<T>& e, T* p) {
+    uint4* q = reinterpret_cast<uint4*>(p);
+    const uint4* d = reinterpret_cast<const uint4*>(e.v);
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(T) * 8 / 16); ++i) q[i] = d[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) p[i] = e.v[i];
-    }
+    for (int i = 0; i < (int)(sizeof(T) * 8 / 16); ++i) q[i] = d[i];
 }
 // Two values into places i and i + 1.
 __device__ __forceinline__ void put2(Eight<float>& e, int i, float a, float b) { e.v[i] = a, e.v[i + 1] = b; }
