@@ -595,6 +595,14 @@ SBNN_API sbnn_status sbnn_debug_mobilenet_v1_launches(const sbnn_mbv1* net, int 
 SBNN_API sbnn_status sbnn_debug_mobilenet_v1_block(sbnn_mbv1* net, int block, const float* in_dev, float* out_dev, int N, int tile, int split,
                                                    void* cuda_stream);
 /*
+ * Test hook: what sbnn_conv1x1_mxfp4 without (activations = 1) and with a workspace (2), or sbnn_conv1x1_mxfp4_q (0), would run
+ * such a call on, on a device of `sms` SMs (host arithmetic only).  *pair: 1 for pairs of CTAs on 256 x 256 tiles; else *pixels of a
+ * tile and the *split CTAs that share its channel steps; *rounds: 1 where these round the activations themselves;
+ * *shared_bytes: shared memory of a CTA (0 for pairs).
+ */
+SBNN_API sbnn_status sbnn_debug_plan_conv1x1_mxfp4(int M, int Cin, int Cout, int y_type, int activations, int sms, int* pair, int* pixels,
+                                                   int* split, int* rounds, int64_t* shared_bytes);
+/*
  * Test hook: from now on the layer's images for the tensor cores are treated as too large for the device where they take more
  * than `bytes`; calls then run on the FMA kernels.
  */

@@ -75,6 +75,7 @@ def lib():
         "sbnn_mxfp4_dequantize": [P, P, P, I, L64, I, I, P],
         "sbnn_conv1x1_mxfp4": [P, P, P, P, I, L64, P, I, L64, I, I, I, I, P, L64, P],
         "sbnn_conv1x1_mxfp4_q": [P, P, P, P, P, P, I, L64, I, I, I, I, P],
+        "sbnn_debug_plan_conv1x1_mxfp4": [I, I, I, I, I, I, P, P, P, P, P],
         "sbnn_logprobs": [P, I, L64, I, I, P, I, P, P, I, P, P, P],
         "sbnn_selftest_wait_timeout": [P],
         "sbnn_prepare": [P, I, I, I, I],
@@ -346,6 +347,15 @@ def selftest_fma_rate(iterations, stream=None) -> float:
     flop = C.c_double()
     _check(lib().sbnn_selftest_fma_rate(int(iterations), C.byref(flop), _stream(stream)))
     return flop.value
+
+
+def debug_plan_conv1x1_mxfp4(m, cin, cout, y_type=SBNN_F32, activations=2, sms=148):
+    """Test hook: (pairs, pixels of a tile, CTAs that share it, whether they round the activations, bytes of shared memory) of such a
+    call; activations: 0 in 4-bit form, 1 to be rounded without a workspace, 2 with one."""
+    pair, pixels, split, rounds, shared = C.c_int(), C.c_int(), C.c_int(), C.c_int(), C.c_int64()
+    _check(lib().sbnn_debug_plan_conv1x1_mxfp4(m, cin, cout, y_type, activations, sms, C.byref(pair), C.byref(pixels), C.byref(split), C.byref(rounds),
+                                               C.byref(shared)))
+    return bool(pair.value), pixels.value, split.value, bool(rounds.value), shared.value
 
 
 def debug_set_packed_device(w: Packed, device) -> int:

@@ -67,9 +67,9 @@ __host__ __device__ constexpr int exchange_width(int bn, int split) { return (bn
 // What a launch needs of shared memory, by parts (all multiples of 1024 bytes except the last).
 struct Layout {
     int a, b, sfa, sfb;     // a stage's operands; FUSED: b and sfb are those of one step and all steps of the CTA stay
-    int stage, resident;
+    int stage;
     int exchange;           // what the CTAs of a cluster send each other
-    int total;
+    int64_t resident, total;   // of any number of steps: past 32 bits from 2^20 on, long after no CTA has room for them
 };
 __host__ __device__ inline Layout layout_of(int bn, int stages, int steps, int split, bool fused) {
     const int own = (steps + split - 1) / split;
@@ -79,9 +79,9 @@ __host__ __device__ inline Layout layout_of(int bn, int stages, int steps, int s
     l.sfa = 1024;
     l.sfb = 1024 * ((bn + 127) / 128);
     l.stage = l.a + l.sfa + (fused ? 0 : l.b + l.sfb);
-    l.resident = fused ? own * (l.b + l.sfb) : 0;
+    l.resident = fused ? (int64_t)own * (l.b + l.sfb) : 0;
     l.exchange = split > 1 ? split * exchange_width(bn, split) * 512 : 0;
-    l.total = stages * l.stage + l.resident + l.exchange + 1024 + (int)sizeof(Shared);
+    l.total = l.resident + stages * l.stage + l.exchange + 1024 + (int)sizeof(Shared);
     return l;
 }
 // Columns of tensor memory: sums, then the scales of the stages.
@@ -218,7 +218,7 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     // operands first, scales behind them: the operands of every stage start on 1024 bytes
     uint8_t* const scales = base + a.stages * (l.a + (FUSED ? 0 : l.b));
     const int op_stage = l.a + (FUSED ? 0 : l.b), sf_stage = l.sfa + (FUSED ? 0 : l.sfb);
-    uint8_t* const resident_sf = resident + (l.resident / (l.b + l.sfb)) * l.b;
+    uint8_t* const resident_sf = resident + ((int)l.resident / (l.b + l.sfb)) * l.b;   // (what a launch has of it fits shared memory)
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int tile = blockIdx.x / a.split, rank = a.split > 1 ? (int)cluster_rank() : 0;
@@ -401,6 +401,13 @@ struct Plan {
     int bn, split, stages;
     bool fused, pair;
 };
+// Whether any number of CTAs up to 8 that share a tile's steps holds these few pixels of its steps beside two stages of weights.
+bool can_round_inside(int64_t M, int K) {
+    const int steps = (K + kStep - 1) / kStep;
+    for (int split = 1; M <= kFusedPixels && split <= 8 && split <= steps; ++split)
+        if (layout_of((int)(M + 7) / 8 * 8, 2, steps, split, true).total <= kMaxSmem) return true;
+    return false;
+}
 
 // Microseconds that a launch of this kernel takes, and one of the kernel of CTA pairs, fitted to what they were measured at (their
 // rounding apart): a CTA starts, fills its pipeline and drains in 2.4 + 0.024 BN, a step brings in 17 KB of weights and 136 bytes a
@@ -423,15 +430,16 @@ double pair_us(int64_t M, int Cout, int steps, int y_bytes, int sms) {
 // 0.55 with two CTAs on an SM, and sharing a tile by the exchange; `pixels`: of those that the CTAs round themselves.  One token 8192 ->
 // 8192 shared by 2 10.4, by 4 9.7; 4096 -> 4096 by 2, 4, 8 6.3, 5.5, 6.1; 1024 -> 1000 by 1, 2, 4 3.6, 4.2, 4.1.
 double few_us(int64_t tiles, int steps, int split, int pixels, int sms) {
-    const int own = (steps + split - 1) / split, rounds = (pixels * own * 32 + 1535) / 1536;
+    const int own = (steps + split - 1) / split;
+    const int64_t rounds = ((int64_t)pixels * own * 32 + 1535) / 1536;
     return 2.6 + (split > 1 ? 0.6 + 0.12 * split : 0.0) + own * (tiles * split > sms ? 0.55 : 0.3) * std::max(1.0, (double)(tiles * split) / (2 * sms)) +
-           0.55 * rounds;
+           0.55 * (double)rounds;
 }
 
 // The width of a tile and the number of CTAs that share its steps, all resident at the same time, that take least by the model, or
 // the kernel of pairs.
-Plan plan_for(int64_t M, int Cout, int K, bool raw, int y_bytes) {
-    const int sms = device_sms(), ctiles = (Cout + 127) / 128, steps = (K + kStep - 1) / kStep;
+Plan plan_for(int64_t M, int Cout, int K, bool raw, int y_bytes, int sms) {
+    const int ctiles = (Cout + 127) / 128, steps = (K + kStep - 1) / kStep;
     Plan p = {};
     double best = 1e30;
     if (M <= kFusedPixels) {
@@ -464,6 +472,16 @@ Plan plan_for(int64_t M, int Cout, int K, bool raw, int y_bytes) {
         }
     }
     p.pair = pair_us(M, Cout, steps, y_bytes, sms) < best;
+    return p;
+}
+// The same for activations that the call has to round, and that it has room for in 4 bits or not.
+Plan plan_rounding(int64_t M, int Cout, int K, bool room, int y_bytes, int sms) {
+    const Plan p = plan_for(M, Cout, K, true, y_bytes, sms);
+    // A CTA of a few pixels rounds all that it meets of them.  From three rounds of its threads on a launch ahead, which does it once, is
+    // the quicker way, if there is room for its result: 16, 24 and 32 pixels 8192 -> 8192 12.7, 14.7 and 17.0 us, ahead 12.9, 13.1 and
+    // 13.3; 32 pixels 4096 -> 4096 8.4 and 9.2.  The sums are the same.
+    const int steps = (K + kStep - 1) / kStep;
+    if (p.fused && room && M * ((steps + p.split - 1) / p.split) * 32 > 3 * 1536) return plan_for(M, Cout, K, false, y_bytes, sms);
     return p;
 }
 
@@ -500,6 +518,8 @@ sbnn_status launch(const Args& given, const Plan& p, const uint8_t* w_codes, con
     return SBNN_OK;
 }
 
+int bytes_of(int type) { return type == SBNN_F32 ? 4 : 2; }
+
 sbnn_status check_call(const uint8_t* w_codes, const uint8_t* w_scales, const float* bias, const void* y, int y_type, int64_t ldy, int M, int Cin,
                        int Cout, int flags) {
     if (M < 0 || Cin <= 0 || Cout <= 0) return fail(SBNN_ERR_SHAPE, "bad shape M=%d Cin=%d Cout=%d", M, Cin, Cout);
@@ -532,7 +552,7 @@ extern "C" sbnn_status sbnn_conv1x1_mxfp4_q(const uint8_t* w_codes_dev, const ui
     Args a = {};
     a.w_scales = w_scales_dev, a.x_scales = x_scales_dev, a.bias = bias_dev, a.y = y_dev, a.ldy = ldy, a.y_type = y_type;
     a.M = M, a.Cout = Cout, a.K = Cin, a.relu = flags & SBNN_RELU;
-    return launch(a, plan_for(M, Cout, Cin, false, y_type == SBNN_F32 ? 4 : 2), w_codes_dev, x_codes_dev, static_cast<cudaStream_t>(cuda_stream));
+    return launch(a, plan_for(M, Cout, Cin, false, bytes_of(y_type), device_sms()), w_codes_dev, x_codes_dev, static_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" sbnn_status sbnn_conv1x1_mxfp4(const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, const float* bias_dev, const void* x_dev,
@@ -553,29 +573,41 @@ extern "C" sbnn_status sbnn_conv1x1_mxfp4(const uint8_t* w_codes_dev, const uint
         if (!aligned16(workspace_dev)) return fail(SBNN_ERR_ALIGN, "workspace_dev must be 16-byte aligned");
     }
     if (M == 0) return SBNN_OK;
+    const bool room = workspace_dev && workspace_bytes >= codes + scales && aligned16(workspace_dev);
+    if (!room && !can_round_inside(M, Cin))
+        return fail(SBNN_ERR_NULL, "Cin=%d is too wide to be rounded without a workspace of %lld bytes", Cin, (long long)(codes + scales));
     if ((r = check_device()) != SBNN_OK) return r;
     if ((r = check_device_memory({w_codes_dev, w_scales_dev, bias_dev, x_dev, y_dev, workspace_dev})) != SBNN_OK) return r;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     Args a = {};
     a.w_scales = w_scales_dev, a.bias = bias_dev, a.y = y_dev, a.ldy = ldy, a.y_type = y_type;
     a.M = M, a.Cout = Cout, a.K = Cin, a.relu = flags & SBNN_RELU;
-    const bool room = workspace_dev && workspace_bytes >= codes + scales && aligned16(workspace_dev);
-    const int y_bytes = y_type == SBNN_F32 ? 4 : 2;
-    Plan p = plan_for(M, Cout, Cin, true, y_bytes);
-    // A CTA of a few pixels rounds all that it meets of them.  From three rounds of its threads on a launch ahead, which does it once, is
-    // the quicker way, if there is room for its result: 16, 24 and 32 pixels 8192 -> 8192 12.7, 14.7 and 17.0 us, ahead 12.9, 13.1 and
-    // 13.3; 32 pixels 4096 -> 4096 8.4 and 9.2.  The sums are the same.
-    const int steps = (Cin + kStep - 1) / kStep;
-    if (p.fused && room && (int64_t)M * ((steps + p.split - 1) / p.split) * 32 > 3 * 1536) p = plan_for(M, Cout, Cin, false, y_bytes);
+    const Plan p = plan_rounding(M, Cout, Cin, room, bytes_of(y_type), device_sms());
     if (p.fused) {
         a.x = x_dev, a.ldx = ldx, a.x_type = x_type;
-        a.vec = ldx * (x_type == SBNN_F32 ? 4 : 2) % 16 == 0;
+        a.vec = ldx * bytes_of(x_type) % 16 == 0;
         return launch(a, p, w_codes_dev, nullptr, st);
     }
-    if (!room) return fail(SBNN_ERR_NULL, "Cin=%d is too wide to be rounded without a workspace of %lld bytes", Cin, (long long)(codes + scales));
     uint8_t* const xc = static_cast<uint8_t*>(workspace_dev);
     a.x_scales = xc + codes;
     if ((r = mxfp4_quantize_launch(x_dev, x_type, ldx, xc, xc + codes, M, Cin, st)) != SBNN_OK) return r;
     a.early = 1;
     return launch(a, p, w_codes_dev, xc, st);
+}
+
+extern "C" sbnn_status sbnn_debug_plan_conv1x1_mxfp4(int M, int Cin, int Cout, int y_type, int activations, int sms, int* pair, int* pixels, int* split,
+                                                     int* rounds, int64_t* shared_bytes) {
+    clear_error();
+    if (!pair || !pixels || !split || !rounds || !shared_bytes) return fail(SBNN_ERR_NULL, "the results must not be NULL");
+    const sbnn_status r = check_call(nullptr, nullptr, nullptr, nullptr, y_type, Cout, M, Cin, Cout, 0);
+    if (r != SBNN_OK) return r;
+    if (M == 0 || sms <= 0 || activations < 0 || activations > 2) return fail(SBNN_ERR_SHAPE, "bad call: M=%d sms=%d activations=%d", M, sms, activations);
+    if (activations == 1 && !can_round_inside(M, Cin)) return fail(SBNN_ERR_NULL, "such a call needs a workspace");
+    const Plan p = activations ? plan_rounding(M, Cout, Cin, activations == 2, bytes_of(y_type), sms) : plan_for(M, Cout, Cin, false, bytes_of(y_type), sms);
+    *pair = p.pair;
+    *pixels = p.pair ? 256 : p.bn;
+    *split = p.pair ? 1 : p.split;
+    *rounds = p.fused;
+    *shared_bytes = p.pair ? 0 : layout_of(p.bn, p.stages, (Cin + kStep - 1) / kStep, p.split, p.fused).total;
+    return SBNN_OK;
 }
