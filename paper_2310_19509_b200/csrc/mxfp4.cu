@@ -216,6 +216,7 @@ extern "C" sbnn_status sbnn_mxfp4_bytes(int M, int K, int64_t* codes_bytes, int6
     clear_error();
     if (!codes_bytes || !scales_bytes) return fail(SBNN_ERR_NULL, "codes_bytes and scales_bytes must not be NULL");
     if (M < 0 || K <= 0) return fail(SBNN_ERR_SHAPE, "bad shape M=%d K=%d", M, K);
+    if (K > 1 << 30) return fail(SBNN_ERR_UNSUPPORTED, "K=%d: 2^30 at most", K);
     *codes_bytes = (int64_t)M * 16 * mx_blocks(K);
     *scales_bytes = (((int64_t)M + 127) / 128) * 512 * mx_ktiles(K);
     return SBNN_OK;

@@ -66,3 +66,13 @@ def test_plan_refusals():
 
     assert plan(0, 8, 8) == plan(4, 0, 8) == plan(4, 8, 8, 0, 3) == plan(4, 8, 8, 0, 2, 0) == "SBNN_ERR_SHAPE"
     assert plan(4, 2 ** 30 + 1, 8) == plan(4, 8, 8, 9) == "SBNN_ERR_UNSUPPORTED"
+
+
+def test_sizes_of_rows_that_no_call_takes_are_refused():
+    """(Sums of channels and a block's or a tile's rounding pass 2^31 for the last of these.)"""
+    assert sbnn.mxfp4_bytes(1, 2 ** 30) == (2 ** 29, 512 * 2 ** 23)
+    for k in (2 ** 30 + 1, 2 ** 31 - 128, 2 ** 31 - 32, 2 ** 31 - 1):
+        for m in (0, 1, 1000):
+            with pytest.raises(sbnn.SbnnError) as e:
+                sbnn.mxfp4_bytes(m, k)
+            assert e.value.name == "SBNN_ERR_UNSUPPORTED"
