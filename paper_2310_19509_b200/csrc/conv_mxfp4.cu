@@ -21,6 +21,7 @@
 
 #include <algorithm>
 
+#include "cluster.cuh"
 #include "common.h"
 #include "mxfp4.cuh"
 #include "mxfp4_mma.cuh"
@@ -104,9 +105,6 @@ __device__ __forceinline__ void umma_mxf4(uint32_t d, uint64_t a, uint64_t b, ui
 // 512 bytes of scales into 4 columns, the same in each quarter of the lanes.
 __device__ __forceinline__ void scales_to_tmem(uint32_t tmem, uint64_t d) {
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(d) : "memory");
-}
-__device__ __forceinline__ void store_remote(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
 // Polls without regard to the abort flag, a bounded number of times: what is in flight when a CTA gives up has to land first.
@@ -194,12 +192,14 @@ __device__ __forceinline__ void drain(const Out<T>& out, uint32_t tmem, int c0, 
     int c = c0;
     for (; c + 32 <= c1; c += 32) {
         uint32_t v[32];
+        __syncwarp();   // the stores of channels that there are not part the lanes
         tmem_ld(tmem + (uint32_t)c, v);
         tmem_ld_wait();
         out.put(c, v);
     }
     for (; c < c1; c += 8) {
         uint32_t v[8];
+        __syncwarp();
         tmem_ld(tmem + (uint32_t)c, v);
         tmem_ld_wait();
         out.put(c, v);
@@ -365,6 +365,7 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             int owner = c0 / width, first_of_owner = owner * width;
             for (int c = c0; c < c1; c += 8) {
                 uint32_t v[8];
+                __syncwarp();
                 tmem_ld(lanes + (uint32_t)c, v);
                 tmem_ld_wait();
 #pragma unroll
@@ -375,9 +376,7 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 }
             }
         }
-        __syncwarp();
-        cluster_arrive();
-        cluster_wait();
+        cluster_sync();
         if (ok) {
             const float4* const sent = reinterpret_cast<const float4*>(exchange);
             for (int c = warp < 4 ? 0 : 4; c < width && rank * width + c < out.pixels; c += 8) {
@@ -393,6 +392,7 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     }
     tc_fence_before_sync();
     __syncthreads();
+    __syncwarp();
     if (warp == 1) tmem_dealloc(tmem, columns);
 }
 

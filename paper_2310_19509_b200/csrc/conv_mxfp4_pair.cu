@@ -12,6 +12,7 @@
 
 #include <algorithm>
 
+#include "cluster.cuh"
 #include "common.h"
 #include "mxfp4.cuh"
 #include "mxfp4_mma.cuh"
@@ -92,9 +93,14 @@ __device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity, volati
     atomicCAS(status, 0, (int)SBNN_ERR_TIMEOUT);
     return false;
 }
-__device__ __forceinline__ void drain_sync(int group) { asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory"); }
+// The four warps of a group.  (Aligned instructions as well: see cluster.cuh.)
+__device__ __forceinline__ void drain_sync(int group) {
+    __syncwarp();
+    asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
+}
 __device__ __forceinline__ bool drain_any(int group, bool v) {
     uint32_t r;
+    __syncwarp();
     asm volatile("{\n\t.reg .pred p, q;\n\t"
                  "setp.ne.b32 p, %1, 0;\n\t"
                  "bar.red.or.pred q, %2, 128, p;\n\t"
@@ -272,6 +278,7 @@ conv_mxfp4_pair_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_co
             for (int h = 0; h < 2; ++h) {
                 const int half = (done & 1) ? h : 1 - h;   // the half that the next tile's sums overlap comes first
                 uint32_t v[2][32];
+                __syncwarp();   // the last stores part the lanes
                 tmem_ld(d + (uint32_t)(half * 128), v[0]);
                 tmem_ld(d + (uint32_t)(half * 128 + 32), v[1]);
                 tmem_ld_wait();

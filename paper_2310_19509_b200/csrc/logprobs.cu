@@ -18,6 +18,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "cluster.cuh"
 #include "common.h"
 #include "mxfp4.cuh"
 #include "pipeline.cuh"
@@ -438,20 +439,6 @@ __device__ __forceinline__ void order(Team<NT>& t, int n, int top, int id) {
     else __syncthreads();
 }
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// Stores where the first CTA of the cluster has `p`.
-__device__ __forceinline__ void store_remote(const void* p, uint32_t v) {
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(0));
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
-}
-__device__ __forceinline__ void store_remote(const void* p, unsigned long long v) {
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(0));
-    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
-}
-
 // What is left of a row, or of the part [v0, v1) of it that a CTA has, when every thread has its sums `a` (has: of at least one vector):
 // joins them, finds the most probable classes and, in the first part, writes the answers.  scan(reaches, least), called by whole warps,
 // takes what is least or more out of the shares of the threads that reach the bound.
@@ -511,13 +498,12 @@ __device__ __forceinline__ void finish(Team<NT>& t, const Params& p, const Row<T
             cluster_wait();   // all CTAs of the cluster have begun
             if (warp == 0) {
                 if (lane == 0) {
-                    store_remote(&t.part_sums[part].m, __float_as_uint(a.m));
-                    store_remote(&t.part_sums[part].s, __float_as_uint(a.s));
-                    store_remote(&t.part_sums[part].u, __float_as_uint(a.u));
+                    store_remote(remote_address(smem_u32(&t.part_sums[part].m), 0), __float_as_uint(a.m));
+                    store_remote(remote_address(smem_u32(&t.part_sums[part].s), 0), __float_as_uint(a.s));
+                    store_remote(remote_address(smem_u32(&t.part_sums[part].u), 0), __float_as_uint(a.u));
                 }
-                for (int i = lane; i < p.top; i += 32) store_remote(&t.list[Team<NT>::CAP + part * p.top + i], t.best[i]);
+                for (int i = lane; i < p.top; i += 32) store_remote(remote_address(smem_u32(&t.list[Team<NT>::CAP + part * p.top + i]), 0), t.best[i]);
             }
-            __syncwarp();
             cluster_arrive();
             if (part) return;
             cluster_wait();

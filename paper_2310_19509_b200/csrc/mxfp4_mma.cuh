@@ -1,4 +1,4 @@
-// What the two kernels that multiply microscaled 4-bit operands share: descriptors of block-scaled MMAs, clusters.
+// What the two kernels that multiply microscaled 4-bit operands share: arguments, descriptors of block-scaled MMAs.
 #pragma once
 
 #include <stdint.h>
@@ -38,25 +38,6 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t smem) {
     d |= (uint64_t)(128 >> 4) << 32;   // groups of 8 rows are 128 bytes apart
     d |= (uint64_t)1 << 46;            // descriptor version; no swizzle
     return d;
-}
-
-// All threads of the cluster: what any of them wrote before its arrival, to whose shared memory ever, is visible behind the wait.
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_sync() {
-    cluster_arrive();
-    cluster_wait();
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-// The address that `addr` has in the shared memory of CTA `rank` of the cluster.
-__device__ __forceinline__ uint32_t remote_address(uint32_t addr, int rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
 }
 
 }  // namespace sbnn
