@@ -76,3 +76,10 @@ def test_sizes_of_rows_that_no_call_takes_are_refused():
             with pytest.raises(sbnn.SbnnError) as e:
                 sbnn.mxfp4_bytes(m, k)
             assert e.value.name == "SBNN_ERR_UNSUPPORTED"
+
+
+def test_the_smoke_test_runs_every_kernel_of_the_layer():
+    from __graft_entry__ import FOUR_BIT_LAYERS
+
+    plans = [sbnn.debug_plan_conv1x1_mxfp4(*layer) for layer in FOUR_BIT_LAYERS]
+    assert [p[3] for p in plans] == [True, False, False] and [p[0] for p in plans] == [False, False, True]
