@@ -292,8 +292,14 @@ def head_noalloc(fc: Packed, x, logits, n, hw, stream=None):
 _ELEMENT_TYPES = {}
 
 
-def _type(t):
-    """The SBNN_F32 / F16 / BF16 of a torch tensor."""
+def _type(t, given=None):
+    """The SBNN_F32 / F16 / BF16 of a torch tensor; a raw address goes with a `given` one.  (None has any: the library refuses it.)"""
+    if given is not None:
+        return given
+    if t is None:
+        return SBNN_F32
+    if isinstance(t, int):
+        raise TypeError("a raw address says nothing of its elements: their type goes with it")
     if not _ELEMENT_TYPES:
         import torch
         _ELEMENT_TYPES.update({torch.float32: SBNN_F32, torch.float16: SBNN_F16, torch.bfloat16: SBNN_BF16})
@@ -310,30 +316,36 @@ def mxfp4_bytes(m, k):
     return codes.value, scales.value
 
 
-def mxfp4_quantize(x, ldx, codes, scales, m, k, stream=None):
-    """x: a tensor of fp32, fp16 or bf16, rows of k elements ldx apart; codes and scales: uint8, of mxfp4_bytes(m, k)."""
-    _check(lib().sbnn_mxfp4_quantize(_ptr(x), _type(x), ldx, _ptr(codes), _ptr(scales), m, k, _stream(stream)))
+def mxfp4_quantize(x, ldx, codes, scales, m, k, stream=None, x_type=None):
+    """x: a tensor of fp32, fp16 or bf16 (or an address, and SBNN_F32, SBNN_F16 or SBNN_BF16 as x_type), rows of k elements ldx apart;
+    codes and scales: uint8, of mxfp4_bytes(m, k)."""
+    _check(lib().sbnn_mxfp4_quantize(_ptr(x), _type(x, x_type), ldx, _ptr(codes), _ptr(scales), m, k, _stream(stream)))
 
 
-def mxfp4_dequantize(codes, scales, y, ldy, m, k, stream=None):
-    _check(lib().sbnn_mxfp4_dequantize(_ptr(codes), _ptr(scales), _ptr(y), _type(y), ldy, m, k, _stream(stream)))
+def mxfp4_dequantize(codes, scales, y, ldy, m, k, stream=None, y_type=None):
+    _check(lib().sbnn_mxfp4_dequantize(_ptr(codes), _ptr(scales), _ptr(y), _type(y, y_type), ldy, m, k, _stream(stream)))
 
 
-def conv1x1_mxfp4(w_codes, w_scales, bias, x, ldx, y, ldy, m, cin, cout, flags=SBNN_RELU, workspace=None, stream=None):
-    """1x1 layer on 4-bit weights, activations rounded to 4 bits inside; workspace: uint8, for m > 32 (see sbnn_conv1x1_mxfp4)."""
-    _check(lib().sbnn_conv1x1_mxfp4(_ptr(w_codes), _ptr(w_scales), _ptr(bias), _ptr(x), _type(x), ldx, _ptr(y), _type(y), ldy, m, cin, cout,
-                                    flags, _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream(stream)))
+def conv1x1_mxfp4(w_codes, w_scales, bias, x, ldx, y, ldy, m, cin, cout, flags=SBNN_RELU, workspace=None, stream=None, x_type=None,
+                  y_type=None, workspace_bytes=None):
+    """1x1 layer on 4-bit weights, activations rounded to 4 bits inside; workspace: uint8, for m > 32 (see sbnn_conv1x1_mxfp4).  Addresses
+    in place of tensors go with x_type, y_type and workspace_bytes."""
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.nbytes
+    _check(lib().sbnn_conv1x1_mxfp4(_ptr(w_codes), _ptr(w_scales), _ptr(bias), _ptr(x), _type(x, x_type), ldx, _ptr(y), _type(y, y_type), ldy, m, cin,
+                                    cout, flags, _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
-def conv1x1_mxfp4_q(w_codes, w_scales, bias, x_codes, x_scales, y, ldy, m, cin, cout, flags=SBNN_RELU, stream=None):
+def conv1x1_mxfp4_q(w_codes, w_scales, bias, x_codes, x_scales, y, ldy, m, cin, cout, flags=SBNN_RELU, stream=None, y_type=None):
     """The same on activations that are in 4-bit form already."""
-    _check(lib().sbnn_conv1x1_mxfp4_q(_ptr(w_codes), _ptr(w_scales), _ptr(bias), _ptr(x_codes), _ptr(x_scales), _ptr(y), _type(y), ldy, m, cin,
-                                      cout, flags, _stream(stream)))
+    _check(lib().sbnn_conv1x1_mxfp4_q(_ptr(w_codes), _ptr(w_scales), _ptr(bias), _ptr(x_codes), _ptr(x_scales), _ptr(y), _type(y, y_type), ldy, m,
+                                      cin, cout, flags, _stream(stream)))
 
 
-def logprobs(logits, ld, rows, classes, targets, ntargets, logprob, entropy, top, top_index, top_logprob, stream=None):
-    """Log probabilities of `targets` (int32 [rows][ntargets]), entropy and the `top` most probable classes of rows of logits."""
-    _check(lib().sbnn_logprobs(_ptr(logits), _type(logits), ld, rows, classes, _ptr(targets), ntargets, _ptr(logprob), _ptr(entropy), top,
+def logprobs(logits, ld, rows, classes, targets, ntargets, logprob, entropy, top, top_index, top_logprob, stream=None, logits_type=None):
+    """Log probabilities of `targets` (int32 [rows][ntargets]), entropy and the `top` most probable classes of rows of logits.  `logits_type`:
+    their type, where they come as an address."""
+    _check(lib().sbnn_logprobs(_ptr(logits), _type(logits, logits_type), ld, rows, classes, _ptr(targets), ntargets, _ptr(logprob), _ptr(entropy), top,
                                _ptr(top_index), _ptr(top_logprob), _stream(stream)))
 
 
