@@ -506,7 +506,8 @@ SBNN_API sbnn_status sbnn_conv1x1_mxfp4_q(const uint8_t* w_codes_dev, const uint
 
 /*
  * What a classifier answers: log probabilities of given classes, entropy and the most probable classes of rows of logits.
- *   logits_dev    [rows] rows of `classes` elements of `type`, ld elements apart (any ld from classes up)
+ *   logits_dev    [rows] rows of `classes` elements of `type`, ld elements apart (any ld from classes up; they may start at any element,
+ *                 the other pointers are 16-byte aligned)
  *   targets_dev   [rows][ntargets] int32 classes; logprob_dev [rows][ntargets] fp32: their log probabilities.  A negative class
  *                 asks for nothing and gets 0; one from `classes` up gets NaN.  Both may be NULL if ntargets = 0.
  *   entropy_dev   [rows] fp32, -sum p log p in nats, or NULL

@@ -693,7 +693,7 @@ template <class T>
 sbnn_status launch_as(const Params& given, cudaStream_t st) {
     Params p = given;
     // vectors of a row at most: one more where rows start anywhere
-    const bool whole = p.ld % Vec<T>::N == 0;
+    const bool whole = p.ld % Vec<T>::N == 0 && aligned16(p.x);
     const int64_t vectors = ((int64_t)p.classes + (whole ? 1 : 2) * (Vec<T>::N - 1)) / Vec<T>::N;
     const int sms = device_sms();
     p.parts = 1;
@@ -745,9 +745,11 @@ extern "C" sbnn_status sbnn_logprobs(const void* logits_dev, int type, int64_t l
         return fail(SBNN_ERR_SHAPE, "top=%d: 0 to %d, and not more than the %d classes", top, kMaxTop, classes);
     if (ntargets && (!targets_dev || !logprob_dev)) return fail(SBNN_ERR_NULL, "targets_dev and logprob_dev must not be NULL");
     if (top && (!top_index_dev || !top_logprob_dev)) return fail(SBNN_ERR_NULL, "top_index_dev and top_logprob_dev must not be NULL");
-    if (!aligned16(logits_dev) || !aligned16(targets_dev) || !aligned16(logprob_dev) || !aligned16(entropy_dev) || !aligned16(top_index_dev) ||
+    if (reinterpret_cast<uintptr_t>(logits_dev) % (type == SBNN_F32 ? 4 : 2))
+        return fail(SBNN_ERR_ALIGN, "logits_dev must lie on a multiple of its elements' size");
+    if (!aligned16(targets_dev) || !aligned16(logprob_dev) || !aligned16(entropy_dev) || !aligned16(top_index_dev) ||
         !aligned16(top_logprob_dev))
-        return fail(SBNN_ERR_ALIGN, "device pointers must be 16-byte aligned");
+        return fail(SBNN_ERR_ALIGN, "targets_dev and the outputs must be 16-byte aligned");
     if (rows == 0) return SBNN_OK;
     sbnn_status r = check_device();
     if (r != SBNN_OK) return r;

@@ -33,3 +33,9 @@ def test_an_address_without_a_type_is_a_type_error():
                  lambda: sbnn.logprobs(P, 9, 4, 9, None, 0, None, None, 0, None, None, stream=0)):
         with pytest.raises(TypeError):
             call()
+
+
+def test_logits_start_at_any_element():
+    for dtype, size in (("float32", 4), ("float16", 2), ("bfloat16", 2)):
+        sbnn.logprobs(T(dtype, at=P + size), 9, 0, 9, None, 0, None, None, 0, None, None, stream=0)
+        assert name(sbnn.logprobs, T(dtype, at=P + size // 2), 9, 4, 9, None, 0, None, None, 0, None, None) == "SBNN_ERR_ALIGN"
