@@ -119,3 +119,17 @@ def test_drawn_and_rising_rows(rows, v, dtype, order):
         x = x.sort(dim=1).values
     targets = torch.randint(v, (rows, 3), generator=torch.Generator().manual_seed(v))
     check(x, dtype, targets, 20)
+
+
+@pytest.mark.parametrize("rows,v", ROWS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("around", [1e6, -1e6])
+def test_logits_around_a_million(rows, v, dtype, around):
+    """Beyond a million differences are taken before they are scaled: shares of a row lie on either side, some far below."""
+    step = 0.0625 if dtype == "f32" else 4096.0
+    g = torch.Generator().manual_seed(v)
+    x = around + step * torch.randint(-40, 41, (rows, v), generator=g).float()
+    x[:, : v // 3] -= 50 * step                       # the first third below the border, or further below it
+    x[:, v // 2::97] = around * 3 if around < 0 else -around
+    targets = torch.randint(v, (rows, 3), generator=g)
+    check(x, dtype, targets, 8)

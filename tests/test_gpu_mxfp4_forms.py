@@ -189,3 +189,45 @@ def test_two_streams_at_once(form):
     torch.cuda.synchronize()
     sbnn.get_async_status()
     assert all(torch.equal(v, want) for side in y for v in side)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_bad_weights_reach_their_channel_and_no_other(form):
+    """Blocks of NaN in the first, a middle and the last output channel."""
+    m, k, n = FORMS[form][0]
+    w, x, xc, xs, ref, s = layer_of(form)
+    want = call(w, x, xc, xs, m, k, n, "f32")
+    bad = sorted({0, n // 2, n - 1})
+    kept = w.scales
+    w.scales = kept.clone()
+    off = O.scale_offsets(n, k)
+    for r, b in zip(bad, (0, off.shape[1] - 1, off.shape[1] // 2)):
+        w.scales[int(off[r, b])] = 255
+    try:
+        got = call(w, x, xc, xs, m, k, n, "f32")
+    finally:
+        w.scales = kept
+    at = torch.tensor(bad, device="cuda")
+    assert bool(got[:, at].isnan().all())
+    keep = torch.ones(n, dtype=torch.bool, device="cuda")
+    keep[at] = False
+    assert torch.equal(got[:, keep], want[:, keep])
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("ex", [-118, -90, 90, 110])
+def test_scales_of_opposite_ends(form, ex):
+    """Activations times 2^ex and weights over 2^ex: the same products, whose scales lie near the ends of their range, and so the same bits."""
+    m, k, n = FORMS[form][0]
+    w, x, xc, xs, ref, s = layer_of(form)
+    want = call(w, x, xc, xs, m, k, n, "f32")
+    kept = w.scales
+    there = (kept != 255) & (kept != 0)               # rows of no channel and blocks behind the last keep their bytes
+    w.scales = torch.where(there, (kept.int() - ex).clamp(0, 254).to(torch.uint8), kept)
+    moved = np.where(xs > 0, xs.astype(np.int64) + ex, 0)
+    assert moved.max() <= 254 and moved[xs > 0].min() >= 0 and int(kept[there].min()) - ex >= 0
+    try:
+        got = call(w, x, xc, moved.astype(np.uint8), m, k, n, "f32", pre=True)
+    finally:
+        w.scales = kept
+    assert torch.equal(got, want)
