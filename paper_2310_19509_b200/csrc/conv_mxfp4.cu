@@ -248,7 +248,7 @@ conv_mxfp4_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = sh.tmem, tmem_sf = tmem + (uint32_t)((a.bn + 31) / 32 * 32);
+    const uint32_t tmem = sh.tmem;
     volatile int* const abort = &sh.abort;
     grid_dependency_release();   // every CTA has its tensor memory: what starts now waits for none of it
     if (warp || !a.early) grid_dependency_wait();

@@ -149,8 +149,8 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
     }
 }
 
-// 16-byte accesses: every row starts on a 16-byte boundary and ends with a whole one.
-bool whole_vectors(const void* p, int64_t ld, int K, int elem_bytes) { return aligned16(p) && ld * elem_bytes % 16 == 0 && K % 8 == 0; }
+// 16-byte accesses: every row starts on a 16-byte boundary, as the matrix does, and ends with a whole one.
+bool whole_vectors(int64_t ld, int K, int elem_bytes) { return ld * elem_bytes % 16 == 0 && K % 8 == 0; }
 
 sbnn_status check_matrix(const char* what, const void* p, int type, int64_t ld, int M, int K) {
     if (M < 0 || K <= 0) return fail(SBNN_ERR_SHAPE, "bad shape M=%d K=%d", M, K);
@@ -181,7 +181,7 @@ sbnn_status quantize_as(const void* x, int64_t ldx, uint8_t* codes, uint8_t* sca
     unsigned blocks;
     const sbnn_status r = grid_of(M, K, &lpr, &blocks);
     if (r != SBNN_OK) return r;
-    auto* const kernel = whole_vectors(x, ldx, K, sizeof(T)) ? quantize_for<T, true>(lpr) : quantize_for<T, false>(lpr);
+    auto* const kernel = whole_vectors(ldx, K, sizeof(T)) ? quantize_for<T, true>(lpr) : quantize_for<T, false>(lpr);
     ChainedLaunchScope chained;
     SBNN_CUDA_TRY(launch_kernel(kernel, dim3(blocks), dim3(kThreads), 0, st, static_cast<const T*>(x), ldx, codes, scales, M, K, mx_ktiles(K)));
     return SBNN_OK;
@@ -192,7 +192,7 @@ sbnn_status dequantize_as(const uint8_t* codes, const uint8_t* scales, void* y, 
     unsigned blocks;
     const sbnn_status r = grid_of(M, K, &lpr, &blocks);
     if (r != SBNN_OK) return r;
-    auto* const kernel = whole_vectors(y, ldy, K, sizeof(T)) ? dequantize_for<T, true>(lpr) : dequantize_for<T, false>(lpr);
+    auto* const kernel = whole_vectors(ldy, K, sizeof(T)) ? dequantize_for<T, true>(lpr) : dequantize_for<T, false>(lpr);
     ChainedLaunchScope chained;
     SBNN_CUDA_TRY(launch_kernel(kernel, dim3(blocks), dim3(kThreads), 0, st, codes, scales, static_cast<T*>(y), ldy, M, K, mx_ktiles(K)));
     return SBNN_OK;
