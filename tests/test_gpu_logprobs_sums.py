@@ -61,7 +61,7 @@ def check(x, dtype, targets, top, ld=None):
 
 
 # By a warp, by 128, 256 and 512 threads that hold a row, by a cluster that holds it or streams it, by a CTA that streams it.
-ROWS = [(1250, 600), (400, 2600), (120, 5000), (200, 16001), (3, 5000), (5, 24001), (300, 20000), (400, 50257), (2, 131072), (40, 131073), (1, 262144)]
+ROWS = [(1250, 600), (400, 2600), (120, 5000), (200, 16001), (3, 5000), (5, 24001), (300, 20000), (160, 50257), (2, 131072), (40, 131073), (1, 262144)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
