@@ -487,7 +487,8 @@ SBNN_API sbnn_status sbnn_mxfp4_dequantize(const uint8_t* codes_dev, const uint8
  *   workspace_dev              device memory for the rounded activations, the two sizes of sbnn_mxfp4_bytes(M, Cin) added; of
  *                              the caller, so that calls in flight at the same time, and graphs, can have their own.  May be NULL
  *                              for M <= SBNN_MXFP4_DIRECT_ROWS and Cin <= SBNN_MXFP4_DIRECT_CHANNELS (some such calls are
- *                              quicker with it; results are the same bits).
+ *                              quicker with it; results are the same bits).  Without it more rows, or rows too wide for shared
+ *                              memory, are refused with SBNN_ERR_NULL.
  * sbnn_conv1x1_mxfp4_q takes activations that are in 4-bit form already (several layers on the same activations round them once).
  * M, Cin and Cout are at most 2^30.  Results below fp32's normal numbers may be lost.
  * A pixel's result does not depend on other pixels' values; the order of its sums depends on M, Cin, Cout and y's type alone.

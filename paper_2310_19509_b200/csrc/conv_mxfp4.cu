@@ -15,8 +15,11 @@
 // Where tiles are fewer than SMs the channel steps of a tile are shared by the CTAs of a cluster, which add up their sums
 // through each other's shared memory in the order of their ranks: results do not depend on timing.
 //
-// Bound: a single token by its weights (8192 -> 8192: 35.7 MB, 5.5 us at the copy rate, of 9.5; the rest is a launch's beginning and
-// end); more pixels by what the L2 delivers, until the kernel of CTA pairs (conv_mxfp4_pair.cu) takes over.
+// Bound: a single token by its weights and by how evenly its CTAs lie on the SMs (8192 -> 8192: 35.7 MB, 5.5 us at the copy rate, of
+// 9.3; -> 32768, 143 MB, more than the L2 holds, 21.8 of 39.7: 128 or 256 equal CTAs fill 86 % of 148 SMs, and the DRAM was at 44 % of its
+// peak at 71 MB; what is fixed is the 3.5 us that 0.5 MB take).  More pixels by what the L2 delivers, until the kernel of
+// CTA pairs (conv_mxfp4_pair.cu) takes over.  Many pixels of few channels by the beginnings and ends of its tiles, which nothing
+// overlaps (802816 pixels 32 -> 64 fp32 214 us of 47, the rounding ahead among them).
 #include <cuda.h>
 
 #include <algorithm>
@@ -412,8 +415,9 @@ bool can_round_inside(int64_t M, int K) {
 // Microseconds that a launch of this kernel takes, and one of the kernel of CTA pairs, fitted to what they were measured at (their
 // rounding apart): a CTA starts, fills its pipeline and drains in 2.4 + 0.024 BN, a step brings in 17 KB of weights and 136 bytes a
 // pixel at 45 bytes a clock and SM, sharing a tile costs the exchange.  300 pixels 4096 -> 4096: tiles of 64 in two waves 18.0 (model
-// 18.0), of pairs 10.4 (11.9); 588, 1024 -> 516 fp32: tiles of 64 shared by two 5.8 (5.5), pairs 8.5 (7.9); 2048, 256 -> 4096:
-// tiles of 256 16.7 (18.0), pairs 11.3 (10.3); 8192, 8192 -> 8192: 327 (316) and 192 (168).
+// 18.2), of pairs 10.4 (12.3); 588, 1024 -> 516 fp32: tiles of 64 shared by two 5.8 (5.6), pairs 8.5 (7.9); 2048, 256 -> 4096:
+// tiles of 256 16.7 (18.4), pairs 11.3 (10.3); 8192, 8192 -> 8192: 327 (409: a step of wide tiles overlaps the next more than the model
+// has it, where pairs are far ahead) and 192 (168).
 double tile_us(int bn) { return 2.4 + 0.024 * bn; }
 double step_us(int bn) { return 0.215 + 0.00168 * bn; }
 double single_us(int64_t tiles, int steps, int bn, int split, int sms) {
