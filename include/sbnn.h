@@ -598,7 +598,7 @@ SBNN_API sbnn_status sbnn_debug_mobilenet_v1_block(sbnn_mbv1* net, int block, co
                                                    void* cuda_stream);
 /*
  * Test hook: what sbnn_conv1x1_mxfp4 without (activations = 1) and with a workspace (2), or sbnn_conv1x1_mxfp4_q (0), would run
- * such a call on, on a device of `sms` SMs (host arithmetic only).  *pair: 1 for pairs of CTAs on 256 x 256 tiles; else *pixels of a
+ * such a call on, on a device of `sms` SMs (2 to 4096; host arithmetic only).  *pair: 1 for pairs of CTAs on 256 x 256 tiles; else *pixels of a
  * tile and the *split CTAs that share its channel steps; *rounds: 1 where these round the activations themselves;
  * *shared_bytes: shared memory of a CTA (0 for pairs).
  */

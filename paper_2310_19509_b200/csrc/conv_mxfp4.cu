@@ -605,7 +605,7 @@ extern "C" sbnn_status sbnn_debug_plan_conv1x1_mxfp4(int M, int Cin, int Cout, i
     if (!pair || !pixels || !split || !rounds || !shared_bytes) return fail(SBNN_ERR_NULL, "the results must not be NULL");
     const sbnn_status r = check_call(nullptr, nullptr, nullptr, nullptr, y_type, Cout, M, Cin, Cout, 0);
     if (r != SBNN_OK) return r;
-    if (M == 0 || sms <= 0 || activations < 0 || activations > 2) return fail(SBNN_ERR_SHAPE, "bad call: M=%d sms=%d activations=%d", M, sms, activations);
+    if (M == 0 || sms < 2 || sms > 4096 || activations < 0 || activations > 2) return fail(SBNN_ERR_SHAPE, "bad call: M=%d sms=%d activations=%d", M, sms, activations);
     if (activations == 1 && !can_round_inside(M, Cin)) return fail(SBNN_ERR_NULL, "such a call needs a workspace");
     const Plan p = activations ? plan_rounding(M, Cout, Cin, activations == 2, bytes_of(y_type), sms) : plan_for(M, Cout, Cin, false, bytes_of(y_type), sms);
     *pair = p.pair;

@@ -64,7 +64,7 @@ def test_plan_refusals():
             sbnn.debug_plan_conv1x1_mxfp4(*a)
         return e.value.name
 
-    assert plan(0, 8, 8) == plan(4, 0, 8) == plan(4, 8, 8, 0, 3) == plan(4, 8, 8, 0, 2, 0) == "SBNN_ERR_SHAPE"
+    assert plan(0, 8, 8) == plan(4, 0, 8) == plan(4, 8, 8, 0, 3) == plan(4, 8, 8, 0, 2, 0) == plan(40, 8, 8, 0, 2, 1) == plan(40, 8, 8, 0, 2, 2 ** 31 - 1) == "SBNN_ERR_SHAPE"
     assert plan(4, 2 ** 30 + 1, 8) == plan(4, 8, 8, 9) == "SBNN_ERR_UNSUPPORTED"
 
 
